@@ -1,0 +1,225 @@
+/*
+ * l3_tokens.h -- C ABI of the operators for models that train on decoded images as packed
+ * patch tokens: images of any sizes cut into square patches, one token each, all images of a
+ * batch end to end in one sequence without padding.  From the decoder's pixels to the tokens
+ * (l3_patch_tokens_batch), and what such a model computes on them next to matrix products:
+ * dropout, positions turned into rotations of queries and keys (with their norms), attention
+ * inside each image, its gradients, and attention for single tokens against a cache.
+ *
+ * The rules of l3.h hold: plain C, an l3_status from every call, all errors synchronous with
+ * nothing enqueued, the caller owns every buffer it passes.  Beyond those:
+ *   - Work is enqueued on `stream` (a hipStream_t, NULL = the default stream) of the context's
+ *     GPU, whichever GPU is current; nothing waits, nothing is allocated, no state is kept between calls
+ *     and nothing of the context is used that two calls could share, so calls of one context may run on
+ *     several streams at once and every call can be captured into a HIP graph, which keeps the
+ *     pointers, sizes and HOST values of the capture and reads DEVICE values anew at every replay.
+ *   - 16-bit elements are of the call's l3_dtype.  Sums, statistics and angles are held in
+ *     32 bits or more, results are rounded once, to nearest even (attention says where it
+ *     rounds in between).
+ *   - Sizes and strides are in elements, not bytes, and strides are non-negative.  Rows of an
+ *     output must not overlap one another, nor inputs unless a call says so.
+ *   - Calls with no work (no tokens, rows or heads) are L3_OK and enqueue nothing.
+ */
+#ifndef L3_TOKENS_H
+#define L3_TOKENS_H
+
+#include "l3.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ------------------------------------------------------------------------
+ * Patch tokens
+ * ------------------------------------------------------------------------ */
+
+typedef struct {
+    const uint8_t* d_rgb;      /* DEVICE: interleaved 8-bit RGB (what l3_decode_batch writes), any alignment */
+    size_t         row_stride; /* bytes between rows, >= 3 * width */
+    uint32_t       width, height;
+} l3_token_image;
+
+#define L3_MAX_PATCH_SIDE 64
+
+/* Cuts n images into patches of side x side pixels, 1 <= side <= L3_MAX_PATCH_SIDE, and writes one
+ * token per patch, all images end to end, the patches of an image row by row:
+ *   d_tokens[t*3*side*side + (c*side + y)*side + x] = (pixel/255 - mean[c]) / stdv[c]
+ * exactly as l3_decode_crop_normalize_batch normalises (l3_normalized_values).  Patches that
+ * reach over the right or lower edge hold 0 there.
+ *   d_tokens     16-byte aligned
+ *   d_positions  DEVICE int32 [tokens][2] or NULL: row and column of each patch in its image
+ *   d_first      DEVICE int32 [n+1] or NULL: each image's first token, then the number of tokens
+ *   tokens       how many tokens d_tokens has room for: must be what l3_patch_tokens_count gives
+ * Errors: INVALID_ARG (also: zero sizes, a stride too small, `tokens` wrong, unaligned d_tokens,
+ * zero stdv), LIMIT (2^31 tokens or more), DEVICE. */
+l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n, uint32_t side,
+                                const float mean[3], const float stdv[3], l3_dtype dtype,
+                                void* d_tokens, int64_t tokens, int32_t* d_positions, int32_t* d_first,
+                                void* stream);
+
+/* ceil(width/side) * ceil(height/side); 0 if an argument is 0 or side is too large. */
+int64_t l3_patch_tokens_count(uint32_t width, uint32_t height, uint32_t side);
+
+/* ------------------------------------------------------------------------
+ * Dropout
+ * ------------------------------------------------------------------------ */
+
+/* y[r][c] = (residual[r][c] +) (kept(e) ? x[r][c] * 65536 / (65536 - t) : 0),  e = r*cols + c,
+ * where t = floor(p * 65536 + 1/2) and kept(e) says that the 16 random bits of element e are at
+ * least t.  The mask is nowhere stored: it is a function of (seed, offset, e), and the gradient
+ * is the same call on the gradient with the same seed and offset and no residual (the
+ * residual's gradient is y's).  A dropped element is 0 whatever x holds, NaN and infinity included.
+ *
+ * Random bits: Philox 4x32 with 7 rounds (Salmon, Moraes, Dror, Shaw, SC 2011), key = seed, counter
+ * = (e/8, offset), low words first; element e takes the low (e even) or high half of word
+ * (e mod 8)/2.  Calls that must be independent of each other differ in seed or offset.
+ *   p         0 <= p <= 1; 1 drops all
+ *   d_offset  DEVICE uint64 or NULL: added to `offset` when the kernel runs, so that every
+ *             replay of a captured call can have a mask of its own
+ *   y may be x or residual, with the same stride; no other overlap.  Any strides >= cols, any alignment
+ *   that an element needs.
+ * Errors: INVALID_ARG, LIMIT (rows*cols of 2^62 or more), DEVICE. */
+l3_status l3_dropout(l3_ctx* ctx, const void* d_x, int64_t x_stride, const void* d_residual,
+                     int64_t residual_stride, void* d_y, int64_t y_stride, int64_t rows, int64_t cols,
+                     l3_dtype dtype, double p, uint64_t seed, uint64_t offset, const uint64_t* d_offset,
+                     void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions; norms of queries and keys
+ * ------------------------------------------------------------------------ */
+
+/* A tensor of heads, element (token, head, i) at token*token_stride + head*head_stride + i. */
+typedef struct {
+    void*   d;
+    int64_t token_stride, head_stride;
+} l3_heads;
+
+#define L3_MAX_HEAD_DIM 128
+
+/* The first 2*pairs elements of every head are turned, pair j by the angle
+ *   2 pi * (position * turns[j] mod 2^64) / 2^64,  pair (a, b) -> magnitude * (a cos - b sin, a sin + b cos);
+ * the elements behind them pass through.  Angles are exact to 2^-32 of a turn at any position. */
+typedef struct {
+    int32_t         pairs;         /* 0 .. head_dim/2 */
+    int32_t         axes;          /* 1: one position per token; 2: the first half of the pairs goes by the
+                                      first position, the second half by the second (pairs even) */
+    int32_t         interleaved;   /* 0: pair j is elements j and j + pairs; else 2j and 2j + 1 */
+    float           magnitude;     /* 1, or the factor that goes with a stretched context */
+    const uint64_t* turns;         /* HOST, one per pair (copied before return) */
+    const int32_t*  d_positions;   /* DEVICE [tokens][axes], any values */
+} l3_rotation;
+
+/* The usual table: turns[j] = round(2^64 * f_j / (2 pi)), f_j = base^(-j/pairs).  With factor
+ * > 1 positions are stretched: by it for all pairs if original_length is 0, else pair by pair
+ * (Peng et al., arxiv 2309.00071): f_j * (g + (1-g)/factor), where g rises from 0 to 1 as the pair's turns over
+ * original_length positions do from `slow` to `fast` (1 and 32 are usual).
+ * Host only.  With two axes every axis has a table of its own.  Errors: INVALID_ARG (NULL, pairs
+ * not in 1..64, base <= 1, factor < 1, negative original_length, slow >= fast, any of them not finite). */
+l3_status l3_rotation_turns(int pairs, double base, double factor, double original_length, double slow, double fast, uint64_t* turns);
+
+/* Turns queries and keys of `tokens` tokens (inverse != 0: by the negative angles, which is also
+ * the way of the gradients).  k_heads = 0: queries only.  Outputs may be the inputs, element for element.
+ * head_dim even, 2..L3_MAX_HEAD_DIM.  Any strides and alignment that an element needs; rows of 16-byte
+ * aligned heads are fastest.
+ * Errors: INVALID_ARG, LIMIT (2^31 tokens or more, more than 65535 heads), DEVICE. */
+l3_status l3_rotate(l3_ctx* ctx, const l3_rotation* rotation, int inverse, int64_t tokens, int head_dim,
+                    int q_heads, l3_heads q, l3_heads q_out, int k_heads, l3_heads k, l3_heads k_out,
+                    l3_dtype dtype, void* stream);
+
+/* The same behind a norm of every head: x_i / sqrt(mean(x^2) + eps) * weight_i, then the
+ * rotation.  Weights: DEVICE float [head_dim], one for queries and one for keys.  eps >= 0. */
+l3_status l3_norm_rotate(l3_ctx* ctx, const l3_rotation* rotation, float eps, int64_t tokens, int head_dim,
+                         int q_heads, l3_heads q, const float* d_q_weight, l3_heads q_out,
+                         int k_heads, l3_heads k, const float* d_k_weight, l3_heads k_out,
+                         l3_dtype dtype, void* stream);
+
+/* Gradients of l3_norm_rotate: from its inputs and the gradients of its outputs (q_grad, k_grad)
+ * those of its inputs (q_back, k_back; these may be q_grad and k_grad, element for element) and of the
+ * weights (float [head_dim], written, not added to; with no tokens 0).  Sums run in a fixed
+ * order: the same call gives the same bits.
+ *   d_workspace  DEVICE, L3_NORM_ROTATE_WORKSPACE bytes, 16-byte aligned, no other work's until
+ *                this call's has run */
+#define L3_NORM_ROTATE_WORKSPACE (1024 * 2 * 128 * 4)
+l3_status l3_norm_rotate_backward(l3_ctx* ctx, const l3_rotation* rotation, float eps, int64_t tokens, int head_dim,
+                                  int q_heads, l3_heads q, const float* d_q_weight, l3_heads q_grad,
+                                  l3_heads q_back, float* d_q_weight_grad,
+                                  int k_heads, l3_heads k, const float* d_k_weight, l3_heads k_grad,
+                                  l3_heads k_back, float* d_k_weight_grad,
+                                  l3_dtype dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Attention over packed images
+ * ------------------------------------------------------------------------ */
+
+typedef enum {
+    L3_MASK_DOCUMENT = 0,   /* a query sees every key of its own image */
+    L3_MASK_CAUSAL = 1,     /* ... of those the ones up to itself */
+    L3_MASK_PREFIX = 2      /* ... of those the ones up to itself and the image's first d_prefix[image] */
+} l3_mask;
+
+/* Query i of an image with n queries and m keys stands at position i + m - n of the keys.  Score of
+ * query and key: s = scale * dot(q, k); with cap > 0 s = cap * tanh(s / cap); with slopes
+ * s -= slopes[head] * |position of the query - position of the key|.  Query head h reads key head
+ * h / (q_heads / kv_heads).  A query that sees no key (n > m under the causal mask, an image without keys) gives 0. */
+typedef struct {
+    int32_t        head_dim;             /* a multiple of 8, 8..L3_MAX_HEAD_DIM */
+    int32_t        q_heads, kv_heads;    /* q_heads a multiple of kv_heads */
+    int32_t        images;
+    int64_t        q_tokens, kv_tokens;  /* tokens that the tensors hold, below 2^31 - 2^16 */
+    const int32_t* d_q_first;            /* DEVICE [images+1]: each image's first query, then the end of the last;
+                                            ascending from 0 on.  Tokens behind the last image are not touched.  (A
+                                            table that does not ascend or leaves the tensors gives undefined
+                                            results, but no access outside the tensors.) */
+    const int32_t* d_kv_first;           /* the same for keys and values; NULL: the same table */
+    l3_mask        mask;
+    const int32_t* d_prefix;             /* DEVICE [images], for L3_MASK_PREFIX */
+    float          scale;
+    float          cap;                  /* 0: none */
+    const float*   d_slopes;             /* DEVICE [q_heads] or NULL */
+    l3_dtype       dtype;
+} l3_attention_shape;
+
+/* out = softmax(scores) v for every image, head and query in one pass over the keys; also, if
+ * d_lse is not NULL, float [q_heads][q_tokens] the logarithm of the sum of the exponentials (what the
+ * gradients need; -infinity for a query that sees nothing).  Weights of the softmax are rounded to
+ * the 16-bit type ahead of their product with the values (relative 2^-9 or 2^-12 each); all else is
+ * held in 32 bits.  A key that no query of an image sees does not matter, whatever it holds; one that only some
+ * see should be finite (its products with weights of 0 reach its neighbours in the causal order).
+ * All tensors: 16-byte aligned, strides multiples of 8.
+ * Errors: INVALID_ARG, LIMIT, DEVICE. */
+l3_status l3_attention(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
+                       l3_heads out, float* d_lse, void* stream);
+
+/* Gradients of l3_attention for queries, keys and values, given its inputs, its results out and
+ * d_lse, and the gradient of out.  Gradients of tokens behind the last image are not touched; those of
+ * shared key heads are summed over their query heads.  Every sum runs in a fixed order: the same
+ * call gives the same bits.  Weights and their gradients are rounded to the 16-bit type ahead of
+ * the products.  The slopes get no gradient.
+ *   d_workspace  DEVICE, l3_attention_workspace(shape) bytes, 16-byte aligned, no other work's until
+ *                this call's has run */
+l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
+                                l3_heads out, const float* d_lse, l3_heads out_grad,
+                                l3_heads q_grad, l3_heads k_grad, l3_heads v_grad,
+                                void* d_workspace, size_t workspace_bytes, void* stream);
+size_t l3_attention_workspace(const l3_attention_shape* shape);   /* 0 if the shape is refused */
+
+/* One query token for each of n sequences against caches of keys and values, element (sequence,
+ * position, head, i) of a cache at sequence*sequence_stride + position*heads.token_stride +
+ * head*heads.head_stride + i.  Sequence b holds d_lengths[b] positions (clipped to 0..max_length) and
+ * its query stands at the last; what lies behind is not read.  Scores as above, mask
+ * none.  A sequence of length 0 gives 0.  q and out: token = sequence.
+ *   max_length   what no length exceeds; the caches must have room for it
+ *   d_workspace  DEVICE, l3_attention_step_workspace bytes, 16-byte aligned, no other work's until this
+ *                call's has run
+ * Errors: INVALID_ARG, LIMIT, DEVICE. */
+l3_status l3_attention_step(l3_ctx* ctx, int n, int head_dim, int q_heads, int kv_heads, l3_heads q,
+                            l3_heads k_cache, int64_t k_sequence_stride, l3_heads v_cache, int64_t v_sequence_stride,
+                            const int32_t* d_lengths, int64_t max_length, float scale, float cap,
+                            const float* d_slopes, l3_heads out, l3_dtype dtype,
+                            void* d_workspace, size_t workspace_bytes, void* stream);
+size_t l3_attention_step_workspace(int n, int head_dim, int q_heads, int kv_heads, int64_t max_length);   /* 0 if refused */
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* L3_TOKENS_H */

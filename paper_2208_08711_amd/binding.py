@@ -24,6 +24,9 @@ EXPORTED_SYMBOLS = (
     "l3_normalized_values",
     "l3_ctx_create", "l3_ctx_destroy", "l3_decode_batch", "l3_decode_crop_normalize_batch",
     "l3_decode_crop_normalize_batch_noalloc", "l3_encode_batch", "l3_ablation_encode_cpu", "l3_ablation_decode_batch",
+    "l3_patch_tokens_count", "l3_patch_tokens_batch", "l3_dropout", "l3_rotation_turns", "l3_rotate", "l3_norm_rotate",
+    "l3_norm_rotate_backward", "l3_attention", "l3_attention_workspace", "l3_attention_backward", "l3_attention_step",
+    "l3_attention_step_workspace",
 )
 
 
@@ -60,6 +63,27 @@ _MASK32, _MASK64 = (1 << 32) - 1, (1 << 64) - 1
 
 class _Crop(ctypes.Structure):
     _fields_ = [("x0", ctypes.c_int32), ("y0", ctypes.c_int32), ("flip", ctypes.c_uint8)]
+
+
+class _TokenImage(ctypes.Structure):
+    _fields_ = [("d_rgb", ctypes.c_void_p), ("row_stride", ctypes.c_size_t),
+                ("width", ctypes.c_uint32), ("height", ctypes.c_uint32)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int32), ("axes", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("turns", ctypes.POINTER(ctypes.c_uint64)), ("d_positions", ctypes.c_void_p)]
+
+
+class _AttentionShape(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("images", ctypes.c_int32),
+                ("q_tokens", ctypes.c_int64), ("kv_tokens", ctypes.c_int64), ("d_q_first", ctypes.c_void_p),
+                ("d_kv_first", ctypes.c_void_p), ("mask", ctypes.c_int), ("d_prefix", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float), ("d_slopes", ctypes.c_void_p), ("dtype", ctypes.c_int)]
 
 
 _lib = None
@@ -119,6 +143,29 @@ def _load():
     lib.l3_encode_batch.restype = ctypes.c_int
     lib.l3_encode_batch.argtypes = [ctypes.c_void_p, ctypes.POINTER(_EncodeItem), ctypes.c_int,
                                     ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    i32, i64, ptr, f32, f64 = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double
+    fp, rot, shape = ctypes.POINTER(f32), ctypes.POINTER(_Rotation), ctypes.POINTER(_AttentionShape)
+    lib.l3_patch_tokens_count.restype = i64
+    lib.l3_patch_tokens_count.argtypes = [ctypes.c_uint32] * 3
+    lib.l3_attention_workspace.restype = ctypes.c_size_t
+    lib.l3_attention_workspace.argtypes = [shape]
+    lib.l3_attention_step_workspace.restype = ctypes.c_size_t
+    lib.l3_attention_step_workspace.argtypes = [i32, i32, i32, i32, i64]
+    for name, args in (
+            ("l3_patch_tokens_batch", [ptr, ctypes.POINTER(_TokenImage), i32, ctypes.c_uint32, fp, fp, i32, ptr, i64, ptr, ptr, ptr]),
+            ("l3_dropout", [ptr, ptr, i64, ptr, i64, ptr, i64, i64, i64, i32, f64, ctypes.c_uint64, ctypes.c_uint64, ptr, ptr]),
+            ("l3_rotation_turns", [i32, f64, f64, f64, f64, f64, ctypes.POINTER(ctypes.c_uint64)]),
+            ("l3_rotate", [ptr, rot, i32, i64, i32, i32, _Heads, _Heads, i32, _Heads, _Heads, i32, ptr]),
+            ("l3_norm_rotate", [ptr, rot, f32, i64, i32, i32, _Heads, ptr, _Heads, i32, _Heads, ptr, _Heads, i32, ptr]),
+            ("l3_norm_rotate_backward", [ptr, rot, f32, i64, i32, i32, _Heads, ptr, _Heads, _Heads, ptr,
+                                         i32, _Heads, ptr, _Heads, _Heads, ptr, i32, ptr, ctypes.c_size_t, ptr]),
+            ("l3_attention", [ptr, shape, _Heads, _Heads, _Heads, _Heads, ptr, ptr]),
+            ("l3_attention_backward", [ptr, shape, _Heads, _Heads, _Heads, _Heads, ptr, _Heads, _Heads, _Heads, _Heads, ptr,
+                                       ctypes.c_size_t, ptr]),
+            ("l3_attention_step", [ptr, i32, i32, i32, i32, _Heads, _Heads, i64, _Heads, i64, ptr, i64, f32, f32, ptr, _Heads, i32,
+                                   ptr, ctypes.c_size_t, ptr])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -355,3 +402,257 @@ def encode_batch(ctx, images, files, file_len, patch=0, status=None, stream=None
     _check(_load().l3_encode_batch(ctx.handle, arr, n, ctypes.c_void_p(file_len.data_ptr()),
                                    ctypes.c_void_p(status.data_ptr() if status is not None else None),
                                    _stream_ptr(stream)), "l3_encode_batch")
+
+
+# ---- operators on packed patch tokens (include/l3_tokens.h) -------------------------------------
+#
+# Tensors of heads are [tokens, heads, head_dim] with contiguous heads, any strides otherwise; their
+# type (bfloat16 or float16) is the call's.  The library cannot see a tensor's size: what a call
+# relies on is checked here.
+
+MASK_DOCUMENT, MASK_CAUSAL, MASK_PREFIX = 0, 1, 2
+MAX_PATCH_SIDE, MAX_HEAD_DIM = 64, 128
+_NORM_ROTATE_WORKSPACE = 1024 * 2 * 128 * 4
+
+
+def _half(*tensors):
+    """The l3_dtype that all the tensors have."""
+    import torch
+    kind = {torch.bfloat16: BF16, torch.float16: FP16}.get(tensors[0].dtype)
+    if kind is None or any(t.dtype != tensors[0].dtype for t in tensors):
+        raise ValueError("expected bfloat16 or float16 tensors of one type")
+    return kind
+
+
+def _on_gpu(*tensors):
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or (device is not None and t.device != device):
+            raise ValueError("expected tensors of one GPU")
+        device = t.device
+
+
+def _words(t, kind, count, what):
+    """Address of a contiguous device tensor of `count` elements of a type (None: 0)."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch." + kind or not t.is_contiguous() or t.numel() != count:
+        raise ValueError("%s: expected a contiguous %s tensor of %d elements" % (what, kind, count))
+    return t.data_ptr()
+
+
+def _heads(t, tokens=None, heads=None, head_dim=None):
+    """l3_heads of a [tokens, heads, head_dim] tensor."""
+    shape = tuple(t.shape)
+    if t.dim() != 3 or any(w is not None and w != s for w, s in zip((tokens, heads, head_dim), shape)):
+        raise ValueError("expected [tokens, heads, head_dim] = %s, got %s" % ((tokens, heads, head_dim), shape))
+    if t.stride(2) != 1 and shape[2] > 1 and t.numel():
+        raise ValueError("the elements of a head must lie side by side")
+    # (a dimension of one has no stride to speak of)
+    return _Heads(t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else 0)
+
+
+def _workspace(given, size, like, stream):
+    """The caller's workspace, or one of torch's that lives as long as the stream needs it."""
+    import torch
+    if given is not None:
+        if not given.is_cuda or not given.is_contiguous():
+            raise ValueError("workspace: expected a contiguous device tensor")
+        return given, given.numel() * given.element_size()
+    given = torch.empty(max(size, 16), dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        given.record_stream(stream)
+    return given, given.numel()
+
+
+def patch_tokens_count(width, height, side):
+    return int(_load().l3_patch_tokens_count(int(width), int(height), int(side)))
+
+
+def patch_tokens_batch(ctx, images, side, mean, stdv, tokens, positions=None, first=None, stream=None, row_strides=None):
+    """images: list of uint8 device tensors [H, W, 3] (pixels side by side; rows contiguous unless their
+    strides say otherwise or row_strides is given); tokens: device tensor [total, 3*side*side]; positions: int32
+    [total, 2] or None; first: int32 [len(images) + 1] or None.  Enqueues on `stream` (default: torch's current)."""
+    n = len(images)
+    arr = (_TokenImage * max(n, 1))()
+    for i, image in enumerate(images):
+        if str(image.dtype) != "torch.uint8" or image.dim() != 3 or image.shape[2] != 3 or image.stride(2) != 1 or image.stride(1) != 3:
+            raise ValueError("expected uint8 [H, W, 3] with pixels side by side")
+        arr[i].d_rgb, arr[i].height, arr[i].width = image.data_ptr(), image.shape[0], image.shape[1]
+        arr[i].row_stride = max(image.stride(0), 3 * image.shape[1]) if row_strides is None else row_strides[i]
+    _on_gpu(tokens, positions, first, *images)
+    if tokens.dim() != 2 or not tokens.is_contiguous() or tokens.shape[1] != 3 * side * side:
+        raise ValueError("tokens: expected a contiguous [total, 3*side*side]")
+    m, s = (ctypes.c_float * 3)(*mean), (ctypes.c_float * 3)(*stdv)
+    _check(_load().l3_patch_tokens_batch(
+        ctx.handle, arr, n, side, m, s, _half(tokens), tokens.data_ptr(), tokens.shape[0],
+        _words(positions, "int32", 2 * tokens.shape[0], "positions"), _words(first, "int32", n + 1, "first"), _stream_ptr(stream)),
+        "l3_patch_tokens_batch")
+
+
+def _rows(t, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("expected a tensor of shape %s, got %s" % (tuple(shape), tuple(t.shape)))
+    if t.dim() != 2:
+        if not t.is_contiguous():
+            raise ValueError("expected a contiguous tensor or [rows, cols]")
+        return t.shape[-1] if t.dim() else 1
+    if t.stride(1) != 1 and t.shape[1] > 1 and t.numel():
+        raise ValueError("the elements of a row must lie side by side")
+    return max(t.stride(0), t.shape[1])
+
+
+def dropout(ctx, x, out, p, seed, offset=0, residual=None, device_offset=None, stream=None):
+    """out = (residual +) x with a share p of the elements dropped and the others scaled up.  [rows, cols] with any row
+    stride, or contiguous of any shape.  The gradient: the same call on the gradient, without residual.
+    device_offset: int64 (or uint64) device tensor of one word, added to offset when the kernel runs."""
+    _on_gpu(x, out, residual, device_offset)
+    kind = _half(*(t for t in (x, out, residual) if t is not None))
+    strides = [0 if t is None else _rows(t, x.shape) for t in (x, residual, out)]
+    if device_offset is not None and (device_offset.numel() != 1 or device_offset.element_size() != 8):
+        raise ValueError("device_offset: expected one 64-bit word")
+    cols = x.shape[-1] if x.dim() else 1
+    rows = x.numel() // cols if cols else 0
+    _check(_load().l3_dropout(
+        ctx.handle, x.data_ptr(), strides[0], None if residual is None else residual.data_ptr(), strides[1], out.data_ptr(), strides[2],
+        rows, cols, kind, float(p), int(seed) & _MASK64, int(offset) & _MASK64,
+        None if device_offset is None else device_offset.data_ptr(), _stream_ptr(stream)), "l3_dropout")
+
+
+def rotation_turns(pairs, base=10000.0, factor=1.0, original_length=0.0, slow=1.0, fast=32.0):
+    """l3_rotation_turns: the table of one axis, as a list of integers."""
+    out = (ctypes.c_uint64 * max(int(pairs), 1))()
+    _check(_load().l3_rotation_turns(int(pairs), float(base), float(factor), float(original_length), float(slow), float(fast), out),
+           "l3_rotation_turns")
+    return list(out)
+
+
+class Rotation:
+    """The constant part of an l3_rotation: turns of all pairs (with two axes the first half of them
+    goes by the first position of a token, the second by its second)."""
+
+    def __init__(self, turns, axes=1, interleaved=False, magnitude=1.0):
+        self.pairs, self.axes, self.interleaved, self.magnitude = len(turns), int(axes), bool(interleaved), float(magnitude)
+        if self.pairs > MAX_HEAD_DIM // 2 or self.axes not in (1, 2):
+            raise ValueError("expected at most %d pairs and 1 or 2 axes" % (MAX_HEAD_DIM // 2))
+        self.turns = (ctypes.c_uint64 * max(self.pairs, 1))(*[int(t) for t in turns])
+
+    def _with(self, positions, tokens):
+        where = None
+        if self.pairs:
+            where = _words(positions, "int32", tokens * self.axes, "positions")
+        return ctypes.byref(_Rotation(self.pairs, self.axes, self.interleaved, self.magnitude, self.turns, where))
+
+
+def _side(tokens, head_dim, *tensors):
+    """(heads, l3_heads of each) of tensors of one shape; nothing where the first is None."""
+    if tensors[0] is None:
+        return 0, [_Heads() for _ in tensors]
+    return tensors[0].shape[1], [_heads(t, tokens, tensors[0].shape[1], head_dim) for t in tensors]
+
+
+def rotate(ctx, rotation, positions, q, q_out, k=None, k_out=None, inverse=False, stream=None):
+    """Queries and keys (or one tensor alone) [tokens, heads, head_dim] turned by their positions, int32 [tokens] or
+    [tokens, axes].  inverse=True turns back, which is also the gradients' way."""
+    tensors = [t for t in (q, q_out, k, k_out) if t is not None]
+    _on_gpu(positions, *tensors)
+    tokens, head_dim = q.shape[0], q.shape[2]
+    hq, (a, b) = _side(tokens, head_dim, q, q_out)
+    hk, (c, d) = _side(tokens, head_dim, k, k_out)
+    _check(_load().l3_rotate(ctx.handle, rotation._with(positions, tokens), int(bool(inverse)), tokens, head_dim, hq, a, b, hk, c, d,
+                             _half(*tensors), _stream_ptr(stream)), "l3_rotate")
+
+
+def norm_rotate(ctx, rotation, positions, q, q_weight, q_out, k=None, k_weight=None, k_out=None, eps=1e-6, stream=None):
+    """Every head of the queries and keys normalised, weighted (float32 [head_dim]) and turned."""
+    tensors = [t for t in (q, q_out, k, k_out) if t is not None]
+    _on_gpu(positions, q_weight, k_weight, *tensors)
+    tokens, head_dim = q.shape[0], q.shape[2]
+    hq, (a, b) = _side(tokens, head_dim, q, q_out)
+    hk, (c, d) = _side(tokens, head_dim, k, k_out)
+    _check(_load().l3_norm_rotate(
+        ctx.handle, rotation._with(positions, tokens), float(eps), tokens, head_dim,
+        hq, a, _words(q_weight, "float32", head_dim, "q_weight"), b, hk, c, _words(k_weight, "float32", head_dim, "k_weight"), d,
+        _half(*tensors), _stream_ptr(stream)), "l3_norm_rotate")
+
+
+def norm_rotate_backward(ctx, rotation, positions, q, q_weight, q_grad, q_back, q_weight_grad,
+                         k=None, k_weight=None, k_grad=None, k_back=None, k_weight_grad=None, eps=1e-6, workspace=None, stream=None):
+    """Gradients of norm_rotate: q_grad, k_grad are those of its outputs, q_back, k_back and the weights'
+    (float32 [head_dim]) are written."""
+    tensors = [t for t in (q, q_grad, q_back, k, k_grad, k_back) if t is not None]
+    _on_gpu(positions, q_weight, k_weight, q_weight_grad, k_weight_grad, *tensors)
+    tokens, head_dim = q.shape[0], q.shape[2]
+    hq, (a, b, c) = _side(tokens, head_dim, q, q_grad, q_back)
+    hk, (d, e, f) = _side(tokens, head_dim, k, k_grad, k_back)
+    room, size = _workspace(workspace, _NORM_ROTATE_WORKSPACE, q, stream)
+    _check(_load().l3_norm_rotate_backward(
+        ctx.handle, rotation._with(positions, tokens), float(eps), tokens, head_dim,
+        hq, a, _words(q_weight, "float32", head_dim, "q_weight"), b, c, _words(q_weight_grad, "float32", head_dim, "q_weight_grad"),
+        hk, d, _words(k_weight, "float32", head_dim, "k_weight"), e, f, _words(k_weight_grad, "float32", head_dim, "k_weight_grad"),
+        _half(*tensors), room.data_ptr(), size, _stream_ptr(stream)), "l3_norm_rotate_backward")
+
+
+def _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, kind):
+    images = q_first.numel() - 1
+    if kv_first is None and k.shape[0] != q.shape[0]:
+        raise ValueError("kv_first: queries and keys differ in number")
+    head_dim = q.shape[2]
+    return _AttentionShape(
+        head_dim, q.shape[1], k.shape[1], images, q.shape[0], k.shape[0], _words(q_first, "int32", images + 1, "q_first"),
+        _words(kv_first, "int32", images + 1, "kv_first"), int(mask), _words(prefix, "int32", images, "prefix"),
+        head_dim ** -0.5 if scale is None else float(scale), float(cap), _words(slopes, "float32", q.shape[1], "slopes"), kind)
+
+
+def attention(ctx, q, k, v, out, q_first, kv_first=None, mask=MASK_DOCUMENT, prefix=None, scale=None, cap=0.0, slopes=None, lse=None,
+              stream=None):
+    """q, out: [tokens, q_heads, head_dim]; k, v: [kv_tokens, kv_heads, head_dim]; q_first (and kv_first): int32
+    [images + 1]; prefix: int32 [images]; slopes: float32 [q_heads]; lse: float32 [q_heads, tokens] for the
+    gradients.  scale: default head_dim ** -0.5."""
+    _on_gpu(q, k, v, out, q_first, kv_first, prefix, slopes, lse)
+    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, _half(q, k, v, out))
+    _check(_load().l3_attention(
+        ctx.handle, ctypes.byref(shape), _heads(q), _heads(k, None, None, q.shape[2]), _heads(v, *k.shape), _heads(out, *q.shape),
+        _words(lse, "float32", q.shape[0] * q.shape[1], "lse"), _stream_ptr(stream)), "l3_attention")
+
+
+def attention_backward(ctx, q, k, v, out, lse, out_grad, q_grad, k_grad, v_grad, q_first, kv_first=None, mask=MASK_DOCUMENT, prefix=None,
+                       scale=None, cap=0.0, slopes=None, workspace=None, stream=None):
+    """Gradients of attention(): q_grad, k_grad and v_grad are written."""
+    _on_gpu(q, k, v, out, lse, out_grad, q_grad, k_grad, v_grad, q_first, kv_first, prefix, slopes)
+    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes,
+                             _half(q, k, v, out, out_grad, q_grad, k_grad, v_grad))
+    lib = _load()
+    room, size = _workspace(workspace, lib.l3_attention_workspace(ctypes.byref(shape)), q, stream)
+    _check(lib.l3_attention_backward(
+        ctx.handle, ctypes.byref(shape), _heads(q), _heads(k, None, None, q.shape[2]), _heads(v, *k.shape), _heads(out, *q.shape),
+        _words(lse, "float32", q.shape[0] * q.shape[1], "lse"), _heads(out_grad, *q.shape), _heads(q_grad, *q.shape),
+        _heads(k_grad, *k.shape), _heads(v_grad, *k.shape), room.data_ptr(), size, _stream_ptr(stream)), "l3_attention_backward")
+
+
+def attention_step(ctx, q, k_cache, v_cache, lengths, out, scale=None, cap=0.0, slopes=None, max_length=None, workspace=None, stream=None):
+    """One query a sequence: q, out [n, q_heads, head_dim]; caches [n, room, kv_heads, head_dim]; lengths int32 [n];
+    max_length: what no length exceeds (default: the caches' room)."""
+    _on_gpu(q, k_cache, v_cache, lengths, out, slopes)
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or k_cache.shape[0] != q.shape[0]:
+        raise ValueError("expected caches [n, room, kv_heads, head_dim]")
+    n, hq, head_dim = q.shape
+    room_for = k_cache.shape[1]
+    most = room_for if max_length is None else int(max_length)
+    if most > room_for:
+        raise ValueError("max_length exceeds the caches' room")
+    if k_cache.shape[3] != head_dim:
+        raise ValueError("queries and caches differ in head_dim")
+    caches = []
+    for c in (k_cache, v_cache):
+        if c.stride(3) != 1 and head_dim > 1 and c.numel():
+            raise ValueError("the elements of a head must lie side by side")
+        caches += [_Heads(c.data_ptr(), c.stride(1), c.stride(2)), c.stride(0)]
+    lib = _load()
+    room, size = _workspace(workspace, lib.l3_attention_step_workspace(n, head_dim, hq, k_cache.shape[2], most), q, stream)
+    _check(lib.l3_attention_step(
+        ctx.handle, n, head_dim, hq, k_cache.shape[2], _heads(q), *caches, _words(lengths, "int32", n, "lengths"), most,
+        head_dim ** -0.5 if scale is None else float(scale), float(cap), _words(slopes, "float32", hq, "slopes"), _heads(out, *q.shape),
+        _half(q, k_cache, v_cache, out), room.data_ptr(), size, _stream_ptr(stream)), "l3_attention_step")

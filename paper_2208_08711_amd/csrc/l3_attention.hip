@@ -1,0 +1,930 @@
+/*
+ * Attention over packed images (include/l3_tokens.h): forward, gradients, single tokens against
+ * a cache.  Scores never reach memory: one pass over the keys carries the running maximum and sum of the
+ * softmax, and the gradients work the scores out again from the saved logarithm of the sum.
+ *
+ * All products run on the matrix cores as 32x32x16 steps, with the scores of a tile transposed:
+ * S^T = K Q^T gives a lane 16 keys of ONE query (column = lane & 31), so maxima and sums are a lane's own
+ * but for one exchange between the wave's halves, and P^T sits in registers as the second operand of
+ * O^T = V^T P^T needs it, once the keys of a step are taken in the order in which the lanes hold
+ * them.  V^T comes out of local memory through the transposing read.
+ */
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "l3_ctx.h"
+#include "l3_half.h"
+#include "l3_tokens.h"
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_const_void;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_huge_valf();
+constexpr int kThreads = 256;              /* 4 waves */
+
+/* What lanes read in place of rows and columns that the tensors do not have. */
+__device__ __attribute__((aligned(16))) uint32_t l3_zeros[4];
+
+__device__ __forceinline__ f32x16 mfma(HalfVec<__bf16, 8>::type a, HalfVec<__bf16, 8>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(HalfVec<_Float16, 8>::type a, HalfVec<_Float16, 8>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+/* Row of register r of an accumulator in the wave's half `half`. */
+__device__ __forceinline__ constexpr int acc_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+/* A lane's value combined with the other half's (lane ^ 32). */
+__device__ __forceinline__ float across_max(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float across_sum(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+/* ---- tiles in local memory ---------------------------------------------------------------- */
+
+/* A tile is rows of Tile<DB>::kChunks chunks of 8 elements, for heads of up to 32 * DB elements.  Chunk
+ * c of row r lies at position c ^ swizzle(r): 16 rows of one chunk (a row read) lie in 16 different
+ * places modulo 256 bytes, and so do 4 rows of 4 chunks (a transposing read). */
+template <int DB>
+struct Tile {
+    static constexpr int kChunks = DB <= 1 ? 4 : DB == 2 ? 8 : 16;
+    static constexpr int kPitch = kChunks * 16;        /* bytes */
+    __device__ static constexpr int swizzle(int r) {
+        return kChunks == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : kChunks == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
+    }
+
+    /* Rows row0 .. row0+ROWS-1 of a tensor, of which rows at or behind `end` and columns at or behind
+     * `dim` are taken as 0, straight from memory; THREADS threads take part, `t` is this one. */
+    template <typename T, int ROWS, int THREADS>
+    __device__ static __forceinline__ void fetch(uint8_t* lds, const T* base, int64_t stride, int row0, int end, int dim, int t) {
+        constexpr int kPlaces = ROWS * kChunks;
+        static_assert(kPlaces % 64 == 0 && (kPlaces % THREADS == 0 || kPlaces < THREADS), "whole waves, whole rounds");
+#pragma unroll
+        for (int i = 0; i < (kPlaces + THREADS - 1) / THREADS; ++i) {
+            const int place = i * THREADS + t;
+            if (kPlaces < THREADS && place >= kPlaces) break;
+            const int r = place / kChunks, c = (place % kChunks) ^ swizzle(r);
+            const bool there = row0 + r < end && c * 8 < dim;
+            const void* src = there ? (const void*)(base + (int64_t)(row0 + r) * stride + c * 8) : (const void*)l3_zeros;
+            const int first = i * THREADS + (t & ~63);  /* the wave's lanes write 16 bytes each from here on */
+            __builtin_amdgcn_global_load_lds((global_const_void*)src, (lds_void*)(lds + first * 16), 16, 0, 0);
+        }
+    }
+
+    /* Operand rows: elements 16*step + 8*half .. +7 of row `row` */
+    template <typename T>
+    __device__ static __forceinline__ typename HalfVec<T, 8>::type row(const uint8_t* lds, int row, int step, int half) {
+        const int c = (2 * step + half) ^ swizzle(row);
+        return __builtin_bit_cast(typename HalfVec<T, 8>::type, *(const u32x4*)(lds + row * kPitch + c * 16));
+    }
+
+    /* Operand columns: of column 32*db + (lane & 31) the rows row0 + 4*half + {0..3, 8..11}, the order in
+     * which an accumulator's registers hold them.  row0 is a multiple of 16. */
+    template <typename T>
+    __device__ static __forceinline__ typename HalfVec<T, 8>::type columns(const uint8_t* lds, int row0, int db, int lane) {
+        const int half = lane >> 5;
+        const int c = db * 4 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+        s16x4 part[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = row0 + 8 * u + 4 * half + ((lane & 15) >> 2);
+            const uint8_t* p = lds + r * kPitch + (c ^ swizzle(r)) * 16 + (lane & 1) * 8;
+            part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+        }
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(typename HalfVec<T, 8>::type, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+/* Waits for this wave's fetches; the barrier behind it makes all waves' tiles whole. */
+__device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+/* Registers 8*t .. 8*t+7 of an accumulator as an operand */
+template <typename T>
+__device__ __forceinline__ typename HalfVec<T, 8>::type narrowed(const f32x16& v, int t) {
+    FloatVec<8>::type f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[8 * t + i];
+    return __builtin_convertvector(f, typename HalfVec<T, 8>::type);
+}
+
+/* ---- which image ------------------------------------------------------------------------- */
+
+struct Shape {
+    const int32_t* q_first;
+    const int32_t* kv_first;
+    const int32_t* prefix;
+    const float* slopes;
+    int32_t images, q_tokens, kv_tokens;
+    int32_t head_dim, q_heads, kv_heads, group;
+    int32_t mask;
+    float scale, cap;
+};
+
+struct Place {
+    int image;           /* -1: no tile left */
+    int tile;            /* of that image */
+    int q0, n, k0, m;    /* its first query, queries, first key, keys */
+};
+
+/* A table entry, held inside the tensor whatever the table says. */
+__device__ __forceinline__ int first_of(const int32_t* first, int i, int tokens) { return min(max(first[i], 0), tokens); }
+
+/* Which tile of which image is the launch's tile number `index`, if every image is cut into tiles of
+ * `rows` queries (by_keys: keys)?  64 images at a time, one a lane. */
+__device__ Place find_tile(const Shape& s, int index, int rows, bool by_keys) {
+    const int lane = threadIdx.x & 63;
+    Place p = {-1, 0, 0, 0, 0, 0};
+    const int32_t* const first = by_keys ? s.kv_first : s.q_first;
+    const int tokens = by_keys ? s.kv_tokens : s.q_tokens;
+    int before = 0;
+    for (int i0 = 0; i0 < s.images; i0 += 64) {
+        const int i = i0 + lane;
+        int tiles = 0;
+        if (i < s.images) {
+            const int count = first_of(first, i + 1, tokens) - first_of(first, i, tokens);
+            tiles = count > 0 ? (count + rows - 1) / rows : 0;
+        }
+        int upto = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const unsigned long long behind = __ballot(before + upto > index);
+        if (behind) {
+            const int who = __builtin_ctzll(behind);
+            p.image = __builtin_amdgcn_readfirstlane(i0 + who);
+            p.tile = __builtin_amdgcn_readfirstlane(index - before - (__shfl(upto, who) - __shfl(tiles, who)));
+            break;
+        }
+        before += __shfl(upto, 63);
+    }
+    if (p.image >= 0) {
+        p.q0 = first_of(s.q_first, p.image, s.q_tokens);
+        p.n = max(0, first_of(s.q_first, p.image + 1, s.q_tokens) - p.q0);
+        p.k0 = first_of(s.kv_first, p.image, s.kv_tokens);
+        p.m = max(0, first_of(s.kv_first, p.image + 1, s.kv_tokens) - p.k0);
+    }
+    return p;
+}
+
+/* Keys of the image that its query i sees: those below this. */
+__device__ __forceinline__ int seen_by(const Shape& s, const Place& p, int prefix, int i) {
+    if (s.mask == L3_MASK_DOCUMENT) return p.m;
+    const int64_t own = (int64_t)i + p.m - p.n + 1;
+    return (int)max((int64_t)prefix, min(max(own, (int64_t)0), (int64_t)p.m));
+}
+
+__device__ __forceinline__ int prefix_of(const Shape& s, const Place& p) {
+    return s.mask == L3_MASK_PREFIX ? min(max(s.prefix[p.image], 0), p.m) : 0;
+}
+
+/* cap * tanh(x / cap) by the exponential: its error is a few 2^-24 of cap, not of the value. */
+__device__ __forceinline__ float tanh_of(float x) {
+    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+}
+
+/* ---- forward ------------------------------------------------------------------------------ */
+
+/* The running softmax of one query a lane (both halves of the wave hold the same). */
+template <int DB>
+struct Running {
+    f32x16 out[DB];      /* O^T, not yet divided */
+    float top;           /* what exponents are taken against, log2; -inf: nothing seen */
+    float sum;           /* this half's keys only */
+
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) out[d] = f32x16{};
+        top = -kInf;
+        sum = 0.0f;
+    }
+};
+
+/* One tile of KEYS keys against 32 queries.  key0: the tile's first key; seen: the keys that this
+ * lane's query sees lie below it (whole: all of the tile does); place: the query's position. */
+template <typename T, int DB, int KEYS, bool CAP, bool SLOPES>
+__device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVec<T, 8>::type (&q)[2 * DB], const uint8_t* k_tile,
+                                         const uint8_t* v_tile, int key0, int seen, bool whole, int place, float scale, float cap,
+                                         float slope, int lane) {
+    constexpr int KB = KEYS / 32;
+    const int half = lane >> 5;
+    f32x16 s[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        s[b] = f32x16{};
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d) s[b] = mfma(Tile<DB>::template row<T>(k_tile, 32 * b + (lane & 31), d, half), q[d], s[b]);
+    }
+    const float factor = CAP || SLOPES ? kLog2e : fmaxf(scale * kLog2e, 0x1p-126f);   /* (-inf stays -inf) */
+    if (CAP || SLOPES) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float v = s[b][r] * scale;
+                if (CAP) v = cap * tanh_of(v / cap);
+                if (SLOPES) v -= slope * fabsf((float)(place - (key0 + 32 * b + acc_row(r, half))));
+                s[b][r] = v;
+            }
+    }
+    if (!whole) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (key0 + 32 * b + acc_row(r, half) >= seen) s[b][r] = -kInf;
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+    most = across_max(most) * factor;
+    if (most != most) most = -kInf;
+    /* The reference point moves only when a maximum outgrows it by 2^8: until then weights of up to 256
+     * are as good as ones of up to 1, and the products so far need no rescaling. */
+    if (__any(most > run.top + 8.0f)) {
+        const float top = fmaxf(run.top, most);
+        const float shrink = run.top > -kInf ? __builtin_amdgcn_exp2f(run.top - top) : 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) run.out[d] *= shrink;
+        run.sum *= shrink;
+        run.top = top;
+    }
+    const float top = run.top > -kInf ? run.top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], factor, -top));
+            sum += s[b][r];
+        }
+    run.sum += sum;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const auto p = narrowed<T>(s[b], t);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                run.out[d] = mfma(Tile<DB>::template columns<T>(v_tile, 32 * b + 16 * t, d, lane), p, run.out[d]);
+        }
+}
+
+struct Heads {
+    const void* d;
+    int64_t token, head;
+};
+
+struct ForwardArgs {
+    Shape s;
+    Heads q, k, v, out;
+    float* lse;
+};
+
+/* A query's head as the second operand: elements 16*d + 8*half .. +7 of the row `lane & 31` stands for */
+template <typename T, int DB>
+__device__ __forceinline__ void load_operand(typename HalfVec<T, 8>::type (&q)[2 * DB], const T* row, bool there, int dim, int half) {
+#pragma unroll
+    for (int d = 0; d < 2 * DB; ++d) {
+        const int c = 16 * d + 8 * half;
+        u32x4 v = {};
+        if (there && c < dim) v = *(const u32x4*)(row + c);
+        q[d] = __builtin_bit_cast(typename HalfVec<T, 8>::type, v);
+    }
+}
+
+constexpr int kQueries = 128;              /* of a workgroup: 32 a wave */
+constexpr int kKeys = 64;                  /* of a tile */
+
+template <typename T, int DB, bool CAP, bool SLOPES>
+__global__ __launch_bounds__(kThreads, 2) void l3_attention_kernel(ForwardArgs a) {
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kKeys * Tile<DB>::kPitch];
+    const Shape& s = a.s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
+    Place p = find_tile(s, index, kQueries, false);
+    if (p.image < 0) return;
+    /* the last queries of an image first: under the causal masks they have the most keys */
+    p.tile = (p.n + kQueries - 1) / kQueries - 1 - p.tile;
+    const int prefix = prefix_of(s, p);
+    const int row0 = p.tile * kQueries + wave * 32, row = row0 + (lane & 31);
+    const int last = min(p.tile * kQueries + kQueries, p.n) - 1;
+    const int all = seen_by(s, p, prefix, last);                 /* keys that any query of the workgroup sees */
+    const int wave_all = row0 < p.n ? seen_by(s, p, prefix, min(row0 + 31, p.n - 1)) : 0;
+    const int wave_whole = row0 < p.n ? seen_by(s, p, prefix, row0) : 0;
+    const int seen = row < p.n ? seen_by(s, p, prefix, row) : 0;
+    const float slope = SLOPES ? s.slopes[head] : 0.0f;
+
+    typename HalfVec<T, 8>::type q[2 * DB];
+    load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)(p.q0 + row) * a.q.token + (int64_t)head * a.q.head, row < p.n, s.head_dim, half);
+    const T* const k = (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head;
+    const T* const v = (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head;
+    Running<DB> run;
+    run.start();
+    const int steps = (all + kKeys - 1) / kKeys;
+    if (steps > 0) {
+        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][0], k, a.k.token, 0, p.m, s.head_dim, threadIdx.x);
+        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][1], v, a.v.token, 0, p.m, s.head_dim, threadIdx.x);
+    }
+    for (int i = 0; i < steps; ++i) {
+        fetched();
+        __syncthreads();
+        const int key0 = i * kKeys;
+        if (i + 1 < steps) {
+            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][0], k, a.k.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
+            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][1], v, a.v.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
+        }
+        if (key0 < wave_all)
+            one_tile<T, DB, kKeys, CAP, SLOPES>(run, q, tiles[i & 1][0], tiles[i & 1][1], key0, seen, key0 + kKeys <= wave_whole,
+                                                row + p.m - p.n, s.scale, s.cap, slope, lane);
+    }
+    if (row >= p.n) return;
+    const float sum = across_sum(run.sum);
+    const float by = seen > 0 ? 1.0f / sum : 0.0f;
+    T* const out = (T*)const_cast<void*>(a.out.d) + (int64_t)(p.q0 + row) * a.out.token + (int64_t)head * a.out.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = 32 * d + 8 * g + 4 * half;
+            if (c >= s.head_dim) continue;
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = seen > 0 ? run.out[d][4 * g + i] * by : 0.0f;
+            store_narrow<T, 4>(out + c, x);
+        }
+    if (a.lse && half == 0) a.lse[(int64_t)head * s.q_tokens + p.q0 + row] = seen > 0 ? (run.top + __builtin_amdgcn_logf(sum)) * kLn2 : -kInf;
+}
+
+/* ---- gradients ----------------------------------------------------------------------------- */
+
+struct BackwardArgs {
+    Shape s;
+    Heads q, k, v, out, out_grad, q_grad, k_grad, v_grad;
+    const float* lse;
+    float* delta;                          /* [q_heads][q_tokens]: dot(out, its gradient) */
+};
+
+/* delta: 16 lanes a head, 8 elements each */
+template <typename T>
+__global__ __launch_bounds__(kThreads) void l3_attention_delta_kernel(BackwardArgs a) {
+    const Shape& s = a.s;
+    const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 16;
+    const int64_t token = at / s.q_heads;
+    const int head = (int)(at - token * s.q_heads), c = (threadIdx.x & 15) * 8;
+    const bool there = token < first_of(s.q_first, s.images, s.q_tokens);
+    float sum = 0.0f;
+    if (there && c < s.head_dim) {
+        float x[8], g[8];
+        load_wide<T, 8>((const T*)a.out.d + token * a.out.token + (int64_t)head * a.out.head + c, x);
+        load_wide<T, 8>((const T*)a.out_grad.d + token * a.out_grad.token + (int64_t)head * a.out_grad.head + c, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], g[i], sum);
+    }
+    for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d);
+    if (there && (threadIdx.x & 15) == 0) a.delta[(int64_t)head * s.q_tokens + token] = sum;
+}
+
+/* The weight of a score (raw product s) and what its gradient is multiplied with on the way to
+ * the raw product, but for the scale. */
+template <bool CAP, bool SLOPES>
+__device__ __forceinline__ float weight_of(float s, float scale, float cap, float slope, int distance, float lse2, float& steep) {
+    steep = 1.0f;
+    if (!CAP && !SLOPES) return __builtin_amdgcn_exp2f(__builtin_fmaf(s, scale * kLog2e, -lse2));
+    float v = s * scale;
+    if (CAP) {
+        const float t = tanh_of(v / cap);
+        v = cap * t;
+        steep = 1.0f - t * t;
+    }
+    if (SLOPES) v -= slope * fabsf((float)distance);
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(v, kLog2e, -lse2));
+}
+
+/* lse in log2; +inf (all weights 0) for a query that sees nothing or is not there */
+__device__ __forceinline__ float lse2_of(const float* lse, int64_t at, bool there) {
+    if (!there) return kInf;
+    const float v = lse[at];
+    return v > -kInf ? v * kLog2e : (v == -kInf ? kInf : v);
+}
+
+/* Gradients of the queries: as the forward, 32 queries a wave, over the keys. */
+template <typename T, int DB, bool CAP, bool SLOPES>
+__global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(BackwardArgs a) {
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kKeys * Tile<DB>::kPitch];
+    const Shape& s = a.s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
+    Place p = find_tile(s, index, kQueries, false);
+    if (p.image < 0) return;
+    p.tile = (p.n + kQueries - 1) / kQueries - 1 - p.tile;
+    const int prefix = prefix_of(s, p);
+    const int row0 = p.tile * kQueries + wave * 32, row = row0 + (lane & 31);
+    const int all = seen_by(s, p, prefix, min(p.tile * kQueries + kQueries, p.n) - 1);
+    const int wave_all = row0 < p.n ? seen_by(s, p, prefix, min(row0 + 31, p.n - 1)) : 0;
+    const int wave_whole = row0 < p.n ? seen_by(s, p, prefix, row0) : 0;
+    const int seen = row < p.n ? seen_by(s, p, prefix, row) : 0;
+    const float slope = SLOPES ? s.slopes[head] : 0.0f;
+    const int place = row + p.m - p.n;
+
+    typename HalfVec<T, 8>::type q[2 * DB], g[2 * DB];
+    load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)(p.q0 + row) * a.q.token + (int64_t)head * a.q.head, row < p.n, s.head_dim, half);
+    load_operand<T, DB>(g, (const T*)a.out_grad.d + (int64_t)(p.q0 + row) * a.out_grad.token + (int64_t)head * a.out_grad.head, row < p.n,
+                        s.head_dim, half);
+    const int64_t at = (int64_t)head * s.q_tokens + p.q0 + row;
+    const float lse2 = lse2_of(a.lse, at, row < p.n), delta = row < p.n ? a.delta[at] : 0.0f;
+    const T* const k = (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head;
+    const T* const v = (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head;
+    f32x16 grad[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) grad[d] = f32x16{};
+    const int steps = (all + kKeys - 1) / kKeys;
+    if (steps > 0) {
+        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][0], k, a.k.token, 0, p.m, s.head_dim, threadIdx.x);
+        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][1], v, a.v.token, 0, p.m, s.head_dim, threadIdx.x);
+    }
+    for (int i = 0; i < steps; ++i) {
+        fetched();
+        __syncthreads();
+        const int key0 = i * kKeys;
+        if (i + 1 < steps) {
+            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][0], k, a.k.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
+            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][1], v, a.v.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
+        }
+        if (key0 >= wave_all) continue;
+        const uint8_t* const k_tile = tiles[i & 1][0];
+        const uint8_t* const v_tile = tiles[i & 1][1];
+        const bool whole = key0 + kKeys <= wave_whole;
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; ++b) {
+            f32x16 x = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < 2 * DB; ++d) {
+                x = mfma(Tile<DB>::template row<T>(k_tile, 32 * b + (lane & 31), d, half), q[d], x);
+                dp = mfma(Tile<DB>::template row<T>(v_tile, 32 * b + (lane & 31), d, half), g[d], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = key0 + 32 * b + acc_row(r, half);
+                float steep;
+                const float w = weight_of<CAP, SLOPES>(x[r], s.scale, s.cap, slope, place - key, lse2, steep);
+                const float ds = w * (dp[r] - delta) * steep;
+                x[r] = whole || key < seen ? ds : 0.0f;
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const auto ds = narrowed<T>(x, t);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) grad[d] = mfma(Tile<DB>::template columns<T>(k_tile, 32 * b + 16 * t, d, lane), ds, grad[d]);
+            }
+        }
+    }
+    if (row >= p.n) return;
+    T* const out = (T*)const_cast<void*>(a.q_grad.d) + (int64_t)(p.q0 + row) * a.q_grad.token + (int64_t)head * a.q_grad.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = 32 * d + 8 * e + 4 * half;
+            if (c >= s.head_dim) continue;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = grad[d][4 * e + i] * s.scale;
+            store_narrow<T, 4>(out + c, y);
+        }
+}
+
+constexpr int kBackKeys = 128;             /* of a workgroup: 32 a wave */
+constexpr int kBackQueries = 32;           /* of a tile */
+
+/* Gradients of keys and values: 32 keys a wave (one a lane), over the queries of all heads that share
+ * them.  S = Q K^T gives a lane 16 queries of its key, and P and dS are second operands of
+ * dV^T = dO^T P and dK^T = Q^T dS as they are. */
+template <typename T, int DB, bool CAP, bool SLOPES>
+__global__ __launch_bounds__(kThreads, 1) void l3_attention_kv_grad_kernel(BackwardArgs a) {
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kBackQueries * Tile<DB>::kPitch];
+    __shared__ float stats[2][2][kBackQueries];
+    const Shape& s = a.s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int index = blockIdx.x / s.kv_heads, kv_head = blockIdx.x - index * s.kv_heads;
+    const Place p = find_tile(s, index, kBackKeys, true);
+    if (p.image < 0) return;
+    const int prefix = prefix_of(s, p);
+    const int tile0 = p.tile * kBackKeys;
+    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31);
+
+    typename HalfVec<T, 8>::type k[2 * DB], v[2 * DB];
+    load_operand<T, DB>(k, (const T*)a.k.d + (int64_t)(p.k0 + key) * a.k.token + (int64_t)kv_head * a.k.head, key < p.m, s.head_dim, half);
+    load_operand<T, DB>(v, (const T*)a.v.d + (int64_t)(p.k0 + key) * a.v.token + (int64_t)kv_head * a.v.head, key < p.m, s.head_dim, half);
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
+
+    /* queries from here on see keys of the workgroup */
+    const int shift = p.m - p.n;
+    int begin = 0;
+    if (s.mask != L3_MASK_DOCUMENT && tile0 >= prefix) begin = min(max(tile0 - shift, 0), p.n) / kBackQueries * kBackQueries;
+    const int per_head = (p.n - begin + kBackQueries - 1) / kBackQueries, steps = per_head * s.group;
+    const auto fetch = [&](int i, int buffer) {
+        const int of = i / per_head, head = kv_head * s.group + of, row0 = begin + (i - of * per_head) * kBackQueries;
+        Tile<DB>::template fetch<T, kBackQueries, kThreads>(
+            tiles[buffer][0], (const T*)a.q.d + (int64_t)p.q0 * a.q.token + (int64_t)head * a.q.head, a.q.token, row0, p.n, s.head_dim, threadIdx.x);
+        Tile<DB>::template fetch<T, kBackQueries, kThreads>(
+            tiles[buffer][1], (const T*)a.out_grad.d + (int64_t)p.q0 * a.out_grad.token + (int64_t)head * a.out_grad.head, a.out_grad.token, row0,
+            p.n, s.head_dim, threadIdx.x);
+        if (threadIdx.x < kBackQueries) {
+            const int row = row0 + (int)threadIdx.x;
+            const int64_t at = (int64_t)head * s.q_tokens + p.q0 + row;
+            stats[buffer][0][threadIdx.x] = lse2_of(a.lse, at, row < p.n);
+            stats[buffer][1][threadIdx.x] = row < p.n ? a.delta[at] : 0.0f;
+        }
+    };
+    if (steps > 0) fetch(0, 0);
+    for (int i = 0; i < steps; ++i) {
+        fetched();
+        __syncthreads();
+        if (i + 1 < steps) fetch(i + 1, (i + 1) & 1);
+        const int of = i / per_head, row0 = begin + (i - of * per_head) * kBackQueries;
+        const float slope = SLOPES ? s.slopes[kv_head * s.group + of] : 0.0f;
+        /* does every query of the tile see every key of the wave?  any? */
+        const bool whole = s.mask == L3_MASK_DOCUMENT || key0 + 31 < seen_by(s, p, prefix, row0);
+        if (s.mask != L3_MASK_DOCUMENT && key0 >= seen_by(s, p, prefix, min(row0 + kBackQueries, p.n) - 1)) continue;
+        const uint8_t* const q_tile = tiles[i & 1][0];
+        const uint8_t* const g_tile = tiles[i & 1][1];
+        f32x16 x = {}, dp = {};
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d) {
+            x = mfma(Tile<DB>::template row<T>(q_tile, lane & 31, d, half), k[d], x);
+            dp = mfma(Tile<DB>::template row<T>(g_tile, lane & 31, d, half), v[d], dp);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int in = acc_row(r, half), row = row0 + in;
+            float steep;
+            float w = weight_of<CAP, SLOPES>(x[r], s.scale, s.cap, slope, row + shift - key, stats[i & 1][0][in], steep);
+            if (!whole && key >= seen_by(s, p, prefix, row)) w = 0.0f;
+            dp[r] = w > 0.0f || w != w ? w * (dp[r] - stats[i & 1][1][in]) * steep : 0.0f;
+            x[r] = w;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const auto w = narrowed<T>(x, t), ds = narrowed<T>(dp, t);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                dv[d] = mfma(Tile<DB>::template columns<T>(g_tile, 16 * t, d, lane), w, dv[d]);
+                dk[d] = mfma(Tile<DB>::template columns<T>(q_tile, 16 * t, d, lane), ds, dk[d]);
+            }
+        }
+    }
+    if (key >= p.m) return;
+    T* const k_out = (T*)const_cast<void*>(a.k_grad.d) + (int64_t)(p.k0 + key) * a.k_grad.token + (int64_t)kv_head * a.k_grad.head;
+    T* const v_out = (T*)const_cast<void*>(a.v_grad.d) + (int64_t)(p.k0 + key) * a.v_grad.token + (int64_t)kv_head * a.v_grad.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = 32 * d + 8 * e + 4 * half;
+            if (c >= s.head_dim) continue;
+            float y[4], z[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = dk[d][4 * e + i] * s.scale;
+                z[i] = dv[d][4 * e + i];
+            }
+            store_narrow<T, 4>(k_out + c, y);
+            store_narrow<T, 4>(v_out + c, z);
+        }
+}
+
+/* ---- single tokens ------------------------------------------------------------------------- */
+
+constexpr int kStepKeys = 32;              /* of a wave's tile */
+constexpr int kStepWaves = 2, kStepThreads = 64 * kStepWaves;
+constexpr int kStepRecord = 2;             /* floats of a partial result ahead of its head_dim: top, sum */
+
+struct StepArgs {
+    Heads q, k, v, out;
+    int64_t k_sequence, v_sequence;
+    const int32_t* lengths;
+    const float* slopes;
+    float* partial;                        /* [sequence][q_heads][chunks] records; nullptr: one chunk, results at once */
+    int32_t n, head_dim, q_heads, kv_heads, group, blocks_of_heads;
+    int32_t max_length, chunk, chunks;     /* keys of a workgroup; workgroups along the longest cache */
+    float scale, cap;
+};
+
+/* A workgroup takes `chunk` keys of one sequence and key head, against up to 32 of the query heads
+ * that share them (one a lane); its waves take tiles in turn, each on its own, and join at the end. */
+template <typename T, int DB, bool CAP, bool SLOPES>
+__global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(StepArgs a) {
+    constexpr int kTile = kStepKeys * Tile<DB>::kPitch;
+    extern __shared__ __attribute__((aligned(256))) uint8_t step_lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    int at = blockIdx.x;
+    const int chunk = at % a.chunks;
+    at /= a.chunks;
+    const int of = at % a.blocks_of_heads;
+    at /= a.blocks_of_heads;
+    const int kv_head = at % a.kv_heads, sequence = at / a.kv_heads;
+    const int length = min(max(a.lengths[sequence], 0), a.max_length);
+    const int begin = chunk * a.chunk, end = min(begin + a.chunk, length);
+    const int in_group = of * 32 + (lane & 31), head = kv_head * a.group + in_group;
+    const bool there = in_group < a.group;
+    if (begin >= length && chunk > 0) return;
+
+    typename HalfVec<T, 8>::type q[2 * DB];
+    load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)sequence * a.q.token + (int64_t)head * a.q.head, there, a.head_dim, half);
+    const float slope = SLOPES && there ? a.slopes[head] : 0.0f;
+    const T* const k = (const T*)a.k.d + (int64_t)sequence * a.k_sequence + (int64_t)kv_head * a.k.head;
+    const T* const v = (const T*)a.v.d + (int64_t)sequence * a.v_sequence + (int64_t)kv_head * a.v.head;
+    uint8_t* const own = step_lds + wave * 4 * kTile;              /* 2 stages of keys and values */
+    Running<DB> run;
+    run.start();
+    const int first = begin + wave * kStepKeys;
+    const auto fetch = [&](int key0, int stage) {
+        Tile<DB>::template fetch<T, kStepKeys, 64>(own + stage * 2 * kTile, k, a.k.token, key0, end, a.head_dim, lane);
+        Tile<DB>::template fetch<T, kStepKeys, 64>(own + stage * 2 * kTile + kTile, v, a.v.token, key0, end, a.head_dim, lane);
+    };
+    if (first < end) fetch(first, 0);
+    int stage = 0;
+    for (int key0 = first; key0 < end; key0 += kStepWaves * kStepKeys, stage ^= 1) {
+        fetched();
+        if (key0 + kStepWaves * kStepKeys < end) fetch(key0 + kStepWaves * kStepKeys, stage ^ 1);
+        one_tile<T, DB, kStepKeys, CAP, SLOPES>(run, q, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, key0 + kStepKeys <= end,
+                                                length - 1, a.scale, a.cap, slope, lane);
+        /* this wave's reads of the tile have come back before the next fetch into it is sent */
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
+    /* join the waves: reference point, sum and products of each through local memory */
+    __syncthreads();
+    float* const tops = (float*)step_lds;                          /* [waves][32], then sums, then products */
+    float* const sums = tops + kStepWaves * 32;
+    float* const products = sums + kStepWaves * 32;                         /* [waves][32 * DB][32] */
+    const float sum = across_sum(run.sum);
+    if (half == 0) {
+        tops[wave * 32 + lane] = run.top;
+        sums[wave * 32 + lane] = sum;
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) products[(wave * 32 * DB + 32 * d + acc_row(r, half)) * 32 + (lane & 31)] = run.out[d][r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * a.head_dim; i += kStepThreads) {
+        const int g = i / a.head_dim, c = i - g * a.head_dim;
+        if (of * 32 + g >= a.group) break;
+        float top = -kInf;
+        for (int w = 0; w < kStepWaves; ++w) top = fmaxf(top, tops[w * 32 + g]);
+        float total = 0.0f, x = 0.0f;
+        for (int w = 0; w < kStepWaves; ++w) {
+            const float f = tops[w * 32 + g] > -kInf ? __builtin_amdgcn_exp2f(tops[w * 32 + g] - top) : 0.0f;
+            total += f * sums[w * 32 + g];
+            x += f * products[(w * 32 * DB + c) * 32 + g];
+        }
+        const int64_t h = kv_head * a.group + of * 32 + g;
+        if (!a.partial) {
+            ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + h * a.out.head + c] = (T)(length > 0 ? x / total : 0.0f);
+            continue;
+        }
+        float* const record = a.partial + (((int64_t)sequence * a.q_heads + h) * a.chunks + chunk) * (a.head_dim + kStepRecord);
+        record[kStepRecord + c] = x;
+        if (c == 0) {
+            record[0] = top;
+            record[1] = total;
+        }
+    }
+}
+
+/* The chunks of a sequence and head joined; one workgroup a head, one thread an element. */
+template <typename T>
+__global__ __launch_bounds__(L3_MAX_HEAD_DIM) void l3_attention_join_kernel(StepArgs a) {
+    const int sequence = blockIdx.x / a.q_heads, head = blockIdx.x - sequence * a.q_heads, c = threadIdx.x;
+    const int length = min(max(a.lengths[sequence], 0), a.max_length);
+    const int chunks = (length + a.chunk - 1) / a.chunk;
+    if (c >= a.head_dim) return;
+    const int64_t pitch = a.head_dim + kStepRecord;
+    const float* const record = a.partial + ((int64_t)sequence * a.q_heads + head) * a.chunks * pitch;
+    float top = -kInf;
+    for (int i = 0; i < chunks; ++i) top = fmaxf(top, record[i * pitch]);
+    float total = 0.0f, x = 0.0f;
+    for (int i = 0; i < chunks; ++i) {
+        const float f = record[i * pitch] > -kInf ? __builtin_amdgcn_exp2f(record[i * pitch] - top) : 0.0f;
+        total += f * record[i * pitch + 1];
+        x += f * record[i * pitch + kStepRecord + c];
+    }
+    ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + (int64_t)head * a.out.head + c] = (T)(chunks > 0 ? x / total : 0.0f);
+}
+
+/* ---- host ---------------------------------------------------------------------------------- */
+
+l3_status launched() { return hipGetLastError() == hipSuccess ? L3_OK : L3_ERR_DEVICE; }
+bool known(l3_dtype dtype) { return dtype == L3_BF16 || dtype == L3_FP16; }
+bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+bool good_heads(const l3_heads& h) {
+    return h.d && aligned(h.d, 16) && h.token_stride >= 0 && h.head_stride >= 0 && h.token_stride % 8 == 0 && h.head_stride % 8 == 0;
+}
+Heads heads_of(const l3_heads& h) { return {h.d, h.token_stride, h.head_stride}; }
+
+bool good_numbers(int head_dim, int q_heads, int kv_heads, float scale, float cap) {
+    return head_dim >= 8 && head_dim <= L3_MAX_HEAD_DIM && head_dim % 8 == 0 && q_heads >= 1 && kv_heads >= 1 &&
+           q_heads % kv_heads == 0 && scale >= 0.0f && std::isfinite(scale) && cap >= 0.0f && std::isfinite(cap);
+}
+
+constexpr int64_t kMostTokens = ((int64_t)1 << 31) - ((int64_t)1 << 16);
+
+/* What a shape is refused for; *nothing: there is no query and no key to work on. */
+l3_status check_shape(const l3_attention_shape* s, bool* nothing) {
+    if (!s || !known(s->dtype) || !good_numbers(s->head_dim, s->q_heads, s->kv_heads, s->scale, s->cap)) return L3_ERR_INVALID_ARG;
+    if (s->mask != L3_MASK_DOCUMENT && s->mask != L3_MASK_CAUSAL && s->mask != L3_MASK_PREFIX) return L3_ERR_INVALID_ARG;
+    if (s->images < 0 || s->q_tokens < 0 || s->kv_tokens < 0) return L3_ERR_INVALID_ARG;
+    if (!s->d_kv_first && s->kv_tokens != s->q_tokens) return L3_ERR_INVALID_ARG;
+    if (s->q_tokens >= kMostTokens || s->kv_tokens >= kMostTokens || s->q_heads > 65535) return L3_ERR_LIMIT;
+    *nothing = s->images == 0 || (s->q_tokens == 0 && s->kv_tokens == 0);
+    if (*nothing) return L3_OK;
+    if (!s->d_q_first || (s->mask == L3_MASK_PREFIX && !s->d_prefix) || !aligned(s->d_q_first, 4) || !aligned(s->d_kv_first, 4) ||
+        !aligned(s->d_prefix, 4) || !aligned(s->d_slopes, 4))
+        return L3_ERR_INVALID_ARG;
+    return L3_OK;
+}
+
+Shape shape_of(const l3_attention_shape& s) {
+    return {s.d_q_first, s.d_kv_first ? s.d_kv_first : s.d_q_first, s.d_prefix, s.d_slopes, s.images, (int32_t)s.q_tokens, (int32_t)s.kv_tokens,
+            s.head_dim, s.q_heads, s.kv_heads, s.q_heads / s.kv_heads, (int32_t)s.mask, s.scale, s.cap};
+}
+
+/* Images of `tokens` tokens in all have at most this many tiles of `rows`. */
+int64_t most_tiles(int64_t tokens, int images, int rows) { return tokens / rows + std::min<int64_t>(images, tokens); }
+
+template <typename F>
+void by_width(int head_dim, F f) {
+    if (head_dim <= 32) f(std::integral_constant<int, 1>());
+    else if (head_dim <= 64) f(std::integral_constant<int, 2>());
+    else if (head_dim <= 96) f(std::integral_constant<int, 3>());
+    else f(std::integral_constant<int, 4>());
+}
+template <typename F>
+void by_score(bool cap, bool slopes, F f) {
+    if (cap && slopes) f(std::true_type(), std::true_type());
+    else if (cap) f(std::true_type(), std::false_type());
+    else if (slopes) f(std::false_type(), std::true_type());
+    else f(std::false_type(), std::false_type());
+}
+
+template <typename T>
+l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
+    const int64_t grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
+    if (grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    by_width(a.s.head_dim, [&](auto db) {
+        by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
+            hipLaunchKernelGGL((l3_attention_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+        });
+    });
+    return launched();
+}
+
+template <typename T>
+l3_status run_backward(const BackwardArgs& a, hipStream_t stream) {
+    const int64_t q_grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
+    const int64_t kv_grid = most_tiles(a.s.kv_tokens, a.s.images, kBackKeys) * a.s.kv_heads;
+    const int64_t delta_grid = ((int64_t)a.s.q_tokens * a.s.q_heads * 16 + kThreads - 1) / kThreads;
+    if (q_grid >= (int64_t)1 << 31 || kv_grid >= (int64_t)1 << 31 || delta_grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    if (delta_grid) hipLaunchKernelGGL((l3_attention_delta_kernel<T>), dim3((unsigned)delta_grid), dim3(kThreads), 0, stream, a);
+    if (launched() != L3_OK) return L3_ERR_DEVICE;
+    by_width(a.s.head_dim, [&](auto db) {
+        by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
+            if (kv_grid)
+                hipLaunchKernelGGL((l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)kv_grid), dim3(kThreads), 0,
+                                   stream, a);
+            if (q_grid)
+                hipLaunchKernelGGL((l3_attention_q_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)q_grid), dim3(kThreads), 0,
+                                   stream, a);
+        });
+    });
+    return launched();
+}
+
+/* How the caches are cut: chunks of whole rounds of the waves, so many that every CU has a few
+ * workgroups, and none so short that joining them would cost more than it gives. */
+void plan_step(int n, int kv_heads, int blocks_of_heads, int64_t max_length, int32_t* chunk, int32_t* chunks) {
+    const int64_t rows = (int64_t)n * kv_heads * blocks_of_heads, wanted = std::max<int64_t>(1, 2048 / rows), round = kStepWaves * kStepKeys;
+    const int64_t each = std::max<int64_t>(4 * round, ((max_length + wanted - 1) / wanted + round - 1) / round * round);
+    *chunk = (int32_t)std::min<int64_t>(each, (int64_t)1 << 30);
+    *chunks = (int32_t)std::max<int64_t>(1, (max_length + *chunk - 1) / *chunk);
+}
+
+template <typename T>
+l3_status run_step(const StepArgs& a, hipStream_t stream) {
+    const int64_t grid = (int64_t)a.n * a.kv_heads * a.blocks_of_heads * a.chunks;
+    if (grid >= (int64_t)1 << 31 || (int64_t)a.n * a.q_heads >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    by_width(a.head_dim, [&](auto db) {
+        by_score(a.cap > 0.0f, a.slopes != nullptr, [&](auto cap, auto slopes) {
+            const size_t tiles = kStepWaves * 4 * (size_t)kStepKeys * Tile<db.value>::kPitch;
+            const size_t join = kStepWaves * (2 * 32 + 32 * db.value * 32) * sizeof(float);
+            const size_t lds = std::max(tiles, join);
+            const auto kernel = l3_attention_step_kernel<T, db.value, cap.value, slopes.value>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kStepThreads), lds, stream, a);
+        });
+    });
+    if (launched() != L3_OK) return L3_ERR_DEVICE;
+    if (a.partial) hipLaunchKernelGGL((l3_attention_join_kernel<T>), dim3((unsigned)(a.n * a.q_heads)), dim3(L3_MAX_HEAD_DIM), 0, stream, a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+l3_status l3_attention(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
+                       l3_heads out, float* d_lse, void* stream) {
+    bool nothing = false;
+    if (!ctx) return L3_ERR_INVALID_ARG;
+    const l3_status status = check_shape(shape, &nothing);
+    if (status != L3_OK) return status;
+    if (nothing || shape->q_tokens == 0) return L3_OK;
+    if (!good_heads(q) || !good_heads(out) || (shape->kv_tokens && (!good_heads(k) || !good_heads(v))) || !aligned(d_lse, 4)) return L3_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    const ForwardArgs a = {shape_of(*shape), heads_of(q), heads_of(k), heads_of(v), heads_of(out), d_lse};
+    return shape->dtype == L3_BF16 ? run_forward<__bf16>(a, (hipStream_t)stream) : run_forward<_Float16>(a, (hipStream_t)stream);
+}
+
+size_t l3_attention_workspace(const l3_attention_shape* shape) {
+    bool nothing = false;
+    if (check_shape(shape, &nothing) != L3_OK) return 0;
+    return ((size_t)shape->q_heads * (size_t)shape->q_tokens * sizeof(float) + 15) / 16 * 16 + 16;
+}
+
+l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
+                                l3_heads out, const float* d_lse, l3_heads out_grad,
+                                l3_heads q_grad, l3_heads k_grad, l3_heads v_grad,
+                                void* d_workspace, size_t workspace_bytes, void* stream) {
+    bool nothing = false;
+    if (!ctx) return L3_ERR_INVALID_ARG;
+    const l3_status status = check_shape(shape, &nothing);
+    if (status != L3_OK) return status;
+    if (nothing) return L3_OK;
+    if (shape->q_tokens && (!good_heads(q) || !good_heads(out) || !good_heads(out_grad) || !good_heads(q_grad) || !d_lse || !aligned(d_lse, 4)))
+        return L3_ERR_INVALID_ARG;
+    if (shape->kv_tokens && (!good_heads(k) || !good_heads(v) || !good_heads(k_grad) || !good_heads(v_grad))) return L3_ERR_INVALID_ARG;
+    if (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < l3_attention_workspace(shape)) return L3_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    const BackwardArgs a = {shape_of(*shape), heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(out_grad), heads_of(q_grad),
+                            heads_of(k_grad), heads_of(v_grad), d_lse, (float*)d_workspace};
+    return shape->dtype == L3_BF16 ? run_backward<__bf16>(a, (hipStream_t)stream) : run_backward<_Float16>(a, (hipStream_t)stream);
+}
+
+size_t l3_attention_step_workspace(int n, int head_dim, int q_heads, int kv_heads, int64_t max_length) {
+    if (n < 0 || max_length < 0 || max_length >= kMostTokens || !good_numbers(head_dim, q_heads, kv_heads, 1.0f, 0.0f)) return 0;
+    if (n == 0) return 16;
+    int32_t chunk, chunks;
+    plan_step(n, kv_heads, (q_heads / kv_heads + 31) / 32, max_length, &chunk, &chunks);
+    return ((size_t)n * q_heads * chunks * (head_dim + kStepRecord) * sizeof(float) + 15) / 16 * 16;
+}
+
+l3_status l3_attention_step(l3_ctx* ctx, int n, int head_dim, int q_heads, int kv_heads, l3_heads q,
+                            l3_heads k_cache, int64_t k_sequence_stride, l3_heads v_cache, int64_t v_sequence_stride,
+                            const int32_t* d_lengths, int64_t max_length, float scale, float cap,
+                            const float* d_slopes, l3_heads out, l3_dtype dtype,
+                            void* d_workspace, size_t workspace_bytes, void* stream) {
+    if (!ctx || !known(dtype) || n < 0 || max_length < 0 || !good_numbers(head_dim, q_heads, kv_heads, scale, cap)) return L3_ERR_INVALID_ARG;
+    if (k_sequence_stride < 0 || v_sequence_stride < 0 || k_sequence_stride % 8 || v_sequence_stride % 8) return L3_ERR_INVALID_ARG;
+    if (max_length >= kMostTokens || q_heads > 65535) return L3_ERR_LIMIT;
+    if (n == 0) return L3_OK;
+    if (!good_heads(q) || !good_heads(out) || (max_length && (!good_heads(k_cache) || !good_heads(v_cache))) || !d_lengths ||
+        !aligned(d_lengths, 4) || !aligned(d_slopes, 4) || !d_workspace || !aligned(d_workspace, 16) ||
+        workspace_bytes < l3_attention_step_workspace(n, head_dim, q_heads, kv_heads, max_length))
+        return L3_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    StepArgs a = {heads_of(q), heads_of(k_cache), heads_of(v_cache), heads_of(out), k_sequence_stride, v_sequence_stride, d_lengths, d_slopes,
+                  (float*)d_workspace, n, head_dim, q_heads, kv_heads, q_heads / kv_heads, (q_heads / kv_heads + 31) / 32, (int32_t)max_length, 0, 0,
+                  scale, cap};
+    plan_step(n, kv_heads, a.blocks_of_heads, max_length, &a.chunk, &a.chunks);
+    if (a.chunks == 1) a.partial = nullptr;
+    return dtype == L3_BF16 ? run_step<__bf16>(a, (hipStream_t)stream) : run_step<_Float16>(a, (hipStream_t)stream);
+}
+
+}  // extern "C"

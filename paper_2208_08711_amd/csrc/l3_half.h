@@ -1,0 +1,43 @@
+/*
+ * 16-bit floats of the operators on packed tokens: vectors of them and their conversion from and
+ * to 32 bits (to nearest even, by the hardware's packed conversions).  Device code only.
+ */
+#ifndef L3_HALF_H
+#define L3_HALF_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace {
+
+template <typename T, int N> struct HalfVec { typedef T type __attribute__((ext_vector_type(N))); };
+template <typename T> struct HalfVec<T, 1> { typedef T type; };
+template <int N> struct FloatVec { typedef float type __attribute__((ext_vector_type(N))); };
+
+/* N elements from memory, widened; p aligned for the vector. */
+template <typename T, int N>
+__device__ __forceinline__ void load_wide(const T* p, float (&out)[N]) {
+    if constexpr (N == 1) {
+        out[0] = (float)*p;
+    } else {
+        const auto v = *reinterpret_cast<const typename HalfVec<T, N>::type*>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = (float)v[i];
+    }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_narrow(T* p, const float (&in)[N]) {
+    if constexpr (N == 1) {
+        *p = (T)in[0];
+    } else {
+        typename FloatVec<N>::type f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = in[i];
+        *reinterpret_cast<typename HalfVec<T, N>::type*>(p) = __builtin_convertvector(f, typename HalfVec<T, N>::type);
+    }
+}
+
+}  // namespace
+
+#endif

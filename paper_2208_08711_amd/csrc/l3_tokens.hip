@@ -1,0 +1,671 @@
+/*
+ * Operators on packed patch tokens that are bound by memory: patch tokens from decoded images,
+ * dropout, rotary positions and norms of queries and keys (include/l3_tokens.h).
+ */
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+
+#include "l3_ctx.h"
+#include "l3_half.h"
+#include "l3_tokens.h"
+
+namespace {
+
+l3_status launched() { return hipGetLastError() == hipSuccess ? L3_OK : L3_ERR_DEVICE; }
+
+bool known(l3_dtype dtype) { return dtype == L3_BF16 || dtype == L3_FP16; }
+
+bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+/* ------------------------------------------------------------------------
+ * Patch tokens
+ * ------------------------------------------------------------------------ */
+
+/* A workgroup takes a strip: up to kStripPixels pixels' width of consecutive patches of one patch
+ * row of one image, whose tokens lie end to end in the output.  The strip's pixel rows come into
+ * local memory as they are; then every lane writes 16 bytes at a time, in the order of the output. */
+constexpr int kTokenThreads = 256;
+constexpr uint32_t kStripPixels = 128;
+constexpr uint32_t kTokenImages = 64;      /* descriptors in the arguments of one launch */
+
+struct TokenImage {
+    const uint8_t* rgb;
+    uint64_t row_stride;
+    uint32_t width, height;
+    uint32_t first_token;
+    uint32_t end_block;                    /* this launch's blocks up to and with this image's */
+};
+
+struct TokenArgs {
+    TokenImage image[kTokenImages];
+    uint16_t table[768];                   /* l3_normalized_values */
+    uint16_t* tokens;
+    int32_t* positions;
+    int32_t* first;
+    uint32_t images, image0, all_images, end_token;
+    uint32_t side, per_strip;              /* patches of a full strip */
+};
+
+__global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArgs a) {
+    extern __shared__ uint8_t lds[];
+    uint16_t* const table = reinterpret_cast<uint16_t*>(lds);
+    uint8_t* const strip = lds + 768 * 2;
+    const uint32_t tid = threadIdx.x;
+
+    /* which image: the first whose blocks end behind this one */
+    uint32_t lo = 0, hi = a.images - 1;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.image[mid].end_block > blockIdx.x) hi = mid; else lo = mid + 1;
+    }
+    const TokenImage im = a.image[lo];
+    const uint32_t block = blockIdx.x - (lo ? a.image[lo - 1].end_block : 0u);
+    const uint32_t side = a.side;
+    const uint32_t cols = (im.width + side - 1) / side;
+    const uint32_t strips = (cols + a.per_strip - 1) / a.per_strip;
+    const uint32_t row = block / strips, col0 = (block - row * strips) * a.per_strip;
+    const uint32_t count = min(a.per_strip, cols - col0);
+    const uint32_t token0 = im.first_token + row * cols + col0;
+
+    for (uint32_t i = tid; i < 768; i += kTokenThreads) table[i] = a.table[i];
+    const uint32_t x0 = col0 * side, y0 = row * side;
+    const uint32_t width = min(count * side, im.width - x0), height = min(side, im.height - y0);   /* inside the image */
+    const uint32_t pitch = a.per_strip * side * 3;
+    const uint32_t bytes = width * 3;
+    for (uint32_t y = tid / 64; y < height; y += kTokenThreads / 64) {
+        const uint8_t* src = im.rgb + (uint64_t)(y0 + y) * im.row_stride + (uint64_t)x0 * 3;
+        for (uint32_t b = tid % 64; b < bytes; b += 64) strip[y * pitch + b] = src[b];
+    }
+    if (a.positions)
+        for (uint32_t t = tid; t < count; t += kTokenThreads) {
+            int32_t* p = a.positions + 2 * (uint64_t)(token0 + t);
+            p[0] = (int32_t)row;
+            p[1] = (int32_t)(col0 + t);
+        }
+    if (a.first && block == 0 && tid == 0) {
+        a.first[a.image0 + lo] = (int32_t)im.first_token;
+        if (a.image0 + lo + 1 == a.all_images) a.first[a.all_images] = (int32_t)a.end_token;
+    }
+    __syncthreads();
+
+    const uint32_t area = side * side, size = 3 * area, total = count * size;
+    uint16_t* const out = a.tokens + (uint64_t)token0 * size;
+    for (uint32_t e0 = tid; e0 < total; e0 += kTokenThreads) {
+        const uint32_t t = e0 / size, r = e0 - t * size;
+        const uint32_t c = r / area, r2 = r - c * area;
+        const uint32_t y = r2 / side, x = t * side + (r2 - y * side);
+        out[e0] = (x < width && y < height) ? table[c * 256 + strip[y * pitch + 3 * x + c]] : (uint16_t)0;
+    }
+}
+
+/* ------------------------------------------------------------------------
+ * Dropout
+ * ------------------------------------------------------------------------ */
+
+struct Philox {
+    uint32_t w[4];
+};
+
+/* Philox 4x32 with 7 rounds (the fewest its authors found to pass every test of BigCrush). */
+__device__ __forceinline__ Philox philox(uint64_t low, uint64_t high, uint64_t key) {
+    uint32_t c0 = (uint32_t)low, c1 = (uint32_t)(low >> 32), c2 = (uint32_t)high, c3 = (uint32_t)(high >> 32);
+    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+#pragma unroll
+    for (int r = 0; r < 7; ++r) {
+        const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c1 = (uint32_t)b;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return {{c0, c1, c2, c3}};
+}
+
+struct DropoutArgs {
+    const void* x;
+    const void* residual;
+    void* y;
+    int64_t x_stride, residual_stride, y_stride, rows, cols;
+    uint64_t seed, offset;
+    const uint64_t* d_offset;
+    float scale;
+    uint32_t threshold;
+};
+
+constexpr int kDropoutThreads = 256;
+
+/* One lane, one counter block: 8 consecutive elements.  WIDE: the rows lie end to end in every
+ * tensor (rows is 1 then) and all are 16-byte aligned. */
+template <typename T, bool WIDE, bool RESIDUAL>
+__global__ __launch_bounds__(kDropoutThreads) void l3_dropout_kernel(DropoutArgs a) {
+    const int64_t count = a.rows * a.cols, blocks = (count + 7) / 8;
+    const uint64_t offset = a.offset + (a.d_offset ? *a.d_offset : 0u);
+    for (int64_t b = (int64_t)blockIdx.x * kDropoutThreads + threadIdx.x; b < blocks; b += (int64_t)gridDim.x * kDropoutThreads) {
+        const int64_t e0 = b * 8;
+        const bool whole = WIDE && e0 + 8 <= count;
+        float x[8], z[8] = {};
+        if (whole) {
+            load_wide<T, 8>((const T*)a.x + e0, x);
+            if (RESIDUAL) load_wide<T, 8>((const T*)a.residual + e0, z);
+        }
+        const Philox random = philox((uint64_t)b, offset, a.seed);
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t bits = (random.w[i / 2] >> (16 * (i & 1))) & 0xFFFFu;
+                z[i] += bits >= a.threshold ? x[i] * a.scale : 0.0f;
+            }
+            store_narrow<T, 8>((T*)a.y + e0, z);
+            continue;
+        }
+        int64_t row = e0 / a.cols, col = e0 - row * a.cols;
+        const int n = (int)min((int64_t)8, count - e0);
+        for (int i = 0; i < n; ++i) {
+            const uint32_t word = i < 4 ? (i < 2 ? random.w[0] : random.w[1]) : (i < 6 ? random.w[2] : random.w[3]);
+            const uint32_t bits = (word >> (16 * (i & 1))) & 0xFFFFu;
+            float v = bits >= a.threshold ? (float)((const T*)a.x)[row * a.x_stride + col] * a.scale : 0.0f;
+            if (RESIDUAL) v += (float)((const T*)a.residual)[row * a.residual_stride + col];
+            ((T*)a.y)[row * a.y_stride + col] = (T)v;
+            if (++col == a.cols) {
+                col = 0;
+                ++row;
+            }
+        }
+    }
+}
+
+template <typename T>
+l3_status launch_dropout(const DropoutArgs& a, bool wide, hipStream_t stream) {
+    const int64_t blocks = (a.rows * a.cols + 8 * kDropoutThreads - 1) / (8 * kDropoutThreads);
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, 256 * 32)), threads(kDropoutThreads);
+    if (a.residual) {
+        if (wide) hipLaunchKernelGGL((l3_dropout_kernel<T, true, true>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((l3_dropout_kernel<T, false, true>), grid, threads, 0, stream, a);
+    } else {
+        if (wide) hipLaunchKernelGGL((l3_dropout_kernel<T, true, false>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((l3_dropout_kernel<T, false, false>), grid, threads, 0, stream, a);
+    }
+    return launched();
+}
+
+/* ------------------------------------------------------------------------
+ * Rotary positions; norms of queries and keys
+ * ------------------------------------------------------------------------ */
+
+/* A head's elements as pairs: pair j < pairs is (j, j + pairs) or, interleaved, (2j, 2j + 1) and is
+ * turned; the others, (2j, 2j + 1), pass through.  A lane takes V consecutive pairs, which are two
+ * runs of V elements; `lanes` lanes (a power of two) take a head, and a slot of them the same pairs of
+ * several heads of one token, so that sines and cosines are worked out once for these. */
+struct RotateTensor {
+    const void* x;
+    void* y;
+    const void* grad;
+    const float* weight;
+    int64_t x_token, x_head, y_token, y_head, grad_token, grad_head;
+    int32_t heads;
+};
+
+struct RotateArgs {
+    RotateTensor t[2];
+    int64_t tokens;
+    const int32_t* positions;
+    float* partial;                        /* backward: [blocks][2][head_dim] */
+    int32_t head_dim, pairs, axes, interleaved, inverse;
+    int32_t lanes, chunks;                 /* lanes of a head; those of them that have pairs */
+    int32_t per_slot, slots_per_token;     /* heads of a slot */
+    float magnitude, eps;
+    uint64_t turns[L3_MAX_HEAD_DIM / 2];
+};
+
+enum { kRotate = 0, kNormRotate = 1, kNormRotateBack = 2 };
+constexpr int kRotateThreads = 256;
+constexpr int kBackBlocks = 1024;          /* most blocks of the backward kernel, which sets the workspace */
+static_assert(L3_NORM_ROTATE_WORKSPACE == kBackBlocks * 2 * L3_MAX_HEAD_DIM * 4, "workspace of the header");
+
+/* Sum over the lanes of a head (every lane gets it). */
+__device__ __forceinline__ float head_sum(float v, int lanes) {
+    for (int s = 1; s < lanes; s <<= 1) v += __shfl_xor(v, s);
+    return v;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_pairs(const T* head, int a, int b, float (&x)[2][V]) {
+    load_wide<T, V>(head + a, x[0]);
+    load_wide<T, V>(head + b, x[1]);
+}
+
+/* The two runs as (first, second) elements of the pairs: as they are in the half layout, every other
+ * element of both runs when pairs lie side by side. */
+template <int V>
+__device__ __forceinline__ void to_pairs(float (&x)[2][V], bool side_by_side) {
+    if (!side_by_side) return;
+    float t[2 * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        t[i] = x[0][i];
+        t[V + i] = x[1][i];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        x[0][i] = t[2 * i];
+        x[1][i] = t[2 * i + 1];
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void from_pairs(float (&x)[2][V], bool side_by_side) {
+    if (!side_by_side) return;
+    float t[2 * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        t[2 * i] = x[0][i];
+        t[2 * i + 1] = x[1][i];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        x[0][i] = t[i];
+        x[1][i] = t[V + i];
+    }
+}
+
+template <typename T, int V, int MODE>
+__global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a) {
+    const int lane = threadIdx.x & (a.lanes - 1);
+    const bool active = lane < a.chunks;
+    const int64_t slots = a.tokens * a.slots_per_token;
+    const int64_t step = (int64_t)gridDim.x * (kRotateThreads / a.lanes);
+    const int j0 = active ? lane * V : 0;                      /* first pair */
+    const bool turned = j0 < a.pairs;
+    const bool side_by_side = !turned || a.interleaved;
+    const int ea = side_by_side ? 2 * j0 : j0;
+    const int eb = side_by_side ? 2 * j0 + V : j0 + a.pairs;
+    uint64_t turns[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) turns[i] = turned ? a.turns[j0 + i] : 0u;
+    const int axis = a.axes == 2 && j0 >= a.pairs / 2 ? 1 : 0;    /* V divides pairs/axes */
+    const int heads = a.t[0].heads + a.t[1].heads;
+    float sum[2][2][V] = {};                                   /* backward: gradients of both weights */
+
+    for (int64_t slot = (int64_t)blockIdx.x * (kRotateThreads / a.lanes) + threadIdx.x / a.lanes; slot < slots; slot += step) {
+        const int64_t token = a.slots_per_token == 1 ? slot : slot / a.slots_per_token;
+        const int h0 = (int)(slot - token * a.slots_per_token) * a.per_slot;
+        const int h1 = min(h0 + a.per_slot, heads);
+        float cs[V], sn[V];
+        const int64_t position = turned ? (int64_t)a.positions[token * a.axes + axis] : 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            /* the product wraps at whole turns; its high half as a signed fraction of a turn is what
+             * the sine and cosine instructions take */
+            const uint64_t angle = (uint64_t)position * turns[i];
+            const float f = (float)(int32_t)(angle >> 32) * 0x1p-32f;
+            const float m = turned ? a.magnitude : 1.0f;
+            cs[i] = __builtin_amdgcn_cosf(f) * m;
+            sn[i] = __builtin_amdgcn_sinf(f) * m;
+            if (a.inverse) sn[i] = -sn[i];
+        }
+        for (int h = h0; h < h1; ++h) {
+            const int which = h >= a.t[0].heads;
+            const RotateTensor& t = a.t[which];
+            const int64_t head = h - (which ? a.t[0].heads : 0);
+            float x[2][V], r[2][V];
+            if (active) load_pairs<T, V>((const T*)t.x + token * t.x_token + head * t.x_head, ea, eb, x);
+            else for (int i = 0; i < V; ++i) x[0][i] = x[1][i] = 0.0f;
+            to_pairs<V>(x, side_by_side);
+            float w[2][V];
+            if (MODE != kRotate) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    w[0][i] = active ? t.weight[side_by_side ? 2 * (j0 + i) : j0 + i] : 0.0f;
+                    w[1][i] = active ? t.weight[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] : 0.0f;
+                }
+                float squares = 0.0f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) squares += x[0][i] * x[0][i] + x[1][i] * x[1][i];
+                const float mean = head_sum(squares, a.lanes) / (float)a.head_dim;
+                const float rstd = 1.0f / sqrtf(mean + a.eps);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    x[0][i] *= rstd;
+                    x[1][i] *= rstd;
+                }
+                if (MODE == kNormRotateBack) {
+                    float g[2][V];
+                    if (active) load_pairs<T, V>((const T*)t.grad + token * t.grad_token + head * t.grad_head, ea, eb, g);
+                    else for (int i = 0; i < V; ++i) g[0][i] = g[1][i] = 0.0f;
+                    to_pairs<V>(g, side_by_side);
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float ga = turned ? g[0][i] * cs[i] - g[1][i] * sn[i] : g[0][i];
+                        const float gb = turned ? g[0][i] * sn[i] + g[1][i] * cs[i] : g[1][i];
+                        sum[0][0][i] += which ? 0.0f : ga * x[0][i];
+                        sum[0][1][i] += which ? 0.0f : gb * x[1][i];
+                        sum[1][0][i] += which ? ga * x[0][i] : 0.0f;
+                        sum[1][1][i] += which ? gb * x[1][i] : 0.0f;
+                        g[0][i] = ga * w[0][i];
+                        g[1][i] = gb * w[1][i];
+                        dot += g[0][i] * x[0][i] + g[1][i] * x[1][i];
+                    }
+                    dot = head_sum(dot, a.lanes) / (float)a.head_dim;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        r[0][i] = rstd * (g[0][i] - x[0][i] * dot);
+                        r[1][i] = rstd * (g[1][i] - x[1][i] * dot);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        x[0][i] *= w[0][i];
+                        x[1][i] *= w[1][i];
+                    }
+                }
+            }
+            if (MODE != kNormRotateBack) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    r[0][i] = turned ? x[0][i] * cs[i] - x[1][i] * sn[i] : x[0][i];
+                    r[1][i] = turned ? x[0][i] * sn[i] + x[1][i] * cs[i] : x[1][i];
+                }
+            }
+            from_pairs<V>(r, side_by_side);
+            if (active) {
+                T* const out = (T*)t.y + token * t.y_token + head * t.y_head;
+                store_narrow<T, V>(out + ea, r[0]);
+                store_narrow<T, V>(out + eb, r[1]);
+            }
+        }
+    }
+
+    if (MODE == kNormRotateBack) {
+        /* every thread's sums into local memory, one column per element, then columns top to bottom */
+        __shared__ float room[kRotateThreads * 2];
+        const int groups = kRotateThreads / a.lanes;
+        for (int which = 0; which < 2; ++which)
+            for (int i = 0; i < V; ++i) {
+                __syncthreads();
+                room[threadIdx.x * 2] = sum[which][0][i];
+                room[threadIdx.x * 2 + 1] = sum[which][1][i];
+                __syncthreads();
+                if ((int)threadIdx.x < a.lanes && active) {
+                    float s0 = 0.0f, s1 = 0.0f;
+                    for (int g = 0; g < groups; ++g) {
+                        s0 += room[(g * a.lanes + lane) * 2];
+                        s1 += room[(g * a.lanes + lane) * 2 + 1];
+                    }
+                    float* const out = a.partial + ((int64_t)blockIdx.x * 2 + which) * a.head_dim;
+                    out[side_by_side ? 2 * (j0 + i) : j0 + i] = s0;
+                    out[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] = s1;
+                }
+            }
+    }
+}
+
+/* Columns of the partial sums: one workgroup per element of one weight. */
+__global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const float* partial, int blocks, int head_dim, float* q, float* k) {
+    __shared__ float room[kRotateThreads];
+    const int column = blockIdx.x;
+    float s = 0.0f;
+    for (int b = threadIdx.x; b < blocks; b += kRotateThreads) s += partial[(int64_t)b * 2 * head_dim + column];
+    room[threadIdx.x] = s;
+    __syncthreads();
+    for (int n = kRotateThreads / 2; n > 0; n >>= 1) {
+        if ((int)threadIdx.x < n) room[threadIdx.x] += room[threadIdx.x + n];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        float* const to = column < head_dim ? q : k;
+        if (to) to[column < head_dim ? column : column - head_dim] = room[0];
+    }
+}
+
+template <typename T, int V>
+void launch_rotate(const RotateArgs& a, int mode, unsigned grid, hipStream_t stream) {
+    const dim3 threads(kRotateThreads);
+    if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate>), dim3(grid), threads, 0, stream, a);
+    else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate>), dim3(grid), threads, 0, stream, a);
+    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack>), dim3(grid), threads, 0, stream, a);
+}
+
+bool good_heads(const l3_heads& h) { return h.d && aligned(h.d, 2) && h.token_stride >= 0 && h.head_stride >= 0; }
+
+/* Are runs of `v` elements of every head aligned for one access? */
+bool wide_heads(const l3_heads& h, int v) {
+    return aligned(h.d, 2 * (size_t)v) && h.token_stride % v == 0 && h.head_stride % v == 0;
+}
+
+struct RotateSide {
+    int heads;
+    l3_heads x, y, grad;
+    const float* weight;
+};
+
+l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps, int64_t tokens, int head_dim,
+                     const RotateSide (&side)[2], int mode, l3_dtype dtype, float* partial, float* q_weight_grad,
+                     float* k_weight_grad, void* stream) {
+    if (!ctx || !rot || !known(dtype) || tokens < 0 || head_dim < 2 || head_dim > L3_MAX_HEAD_DIM || head_dim % 2)
+        return L3_ERR_INVALID_ARG;
+    if (rot->pairs < 0 || 2 * rot->pairs > head_dim || (rot->axes != 1 && rot->axes != 2) || rot->pairs % rot->axes ||
+        !std::isfinite(rot->magnitude) || (rot->pairs && !rot->turns))
+        return L3_ERR_INVALID_ARG;
+    if (side[0].heads < 0 || side[1].heads < 0 || !(eps >= 0.0f) || !std::isfinite(eps)) return L3_ERR_INVALID_ARG;
+    const bool work = tokens > 0 && side[0].heads + side[1].heads > 0;
+    if (work && rot->pairs && !rot->d_positions) return L3_ERR_INVALID_ARG;
+    for (int s = 0; s < 2; ++s) {
+        if (!side[s].heads || !tokens) continue;
+        if (!good_heads(side[s].x) || !good_heads(side[s].y)) return L3_ERR_INVALID_ARG;
+        if (mode != kRotate && !side[s].weight) return L3_ERR_INVALID_ARG;
+        if (mode == kNormRotateBack && !good_heads(side[s].grad)) return L3_ERR_INVALID_ARG;
+    }
+    if (tokens >= (int64_t)1 << 31 || side[0].heads > 65535 || side[1].heads > 65535) return L3_ERR_LIMIT;
+    if (!work && mode != kNormRotateBack) return L3_OK;
+
+    RotateArgs a = {};
+    int v = 8;
+    for (;; v = v == 8 ? 4 : 1) {
+        if (v == 1) break;
+        bool ok = rot->pairs / rot->axes % v == 0 && head_dim / 2 % v == 0;
+        for (int s = 0; s < 2; ++s)
+            if (side[s].heads)
+                ok = ok && wide_heads(side[s].x, v) && wide_heads(side[s].y, v) &&
+                     (mode != kNormRotateBack || wide_heads(side[s].grad, v));
+        if (ok) break;
+    }
+    a.chunks = head_dim / 2 / v;
+    a.lanes = 1;
+    while (a.lanes < a.chunks) a.lanes *= 2;
+    for (int s = 0; s < 2; ++s) {
+        RotateTensor& t = a.t[s];
+        t.x = side[s].x.d;
+        t.y = side[s].y.d;
+        t.grad = side[s].grad.d;
+        t.weight = side[s].weight;
+        t.x_token = side[s].x.token_stride;
+        t.x_head = side[s].x.head_stride;
+        t.y_token = side[s].y.token_stride;
+        t.y_head = side[s].y.head_stride;
+        t.grad_token = side[s].grad.token_stride;
+        t.grad_head = side[s].grad.head_stride;
+        t.heads = side[s].heads;
+    }
+    a.tokens = work ? tokens : 0;
+    a.positions = rot->d_positions;
+    a.partial = partial;
+    a.head_dim = head_dim;
+    a.pairs = rot->pairs;
+    a.axes = rot->axes;
+    a.interleaved = rot->interleaved != 0;
+    a.inverse = (mode == kNormRotateBack) != (inverse != 0);
+    a.magnitude = rot->magnitude;
+    a.eps = eps;
+    if (rot->pairs) std::memcpy(a.turns, rot->turns, (size_t)rot->pairs * 8);
+    const int heads = side[0].heads + side[1].heads;
+    a.per_slot = 1;
+    a.slots_per_token = heads > 0 ? heads : 1;
+    const int64_t slots = a.tokens * a.slots_per_token;
+    int64_t grid = (slots * a.lanes + kRotateThreads - 1) / kRotateThreads;
+    grid = std::max<int64_t>(1, std::min<int64_t>(grid, mode == kNormRotateBack ? kBackBlocks : 16384));
+
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dtype == L3_BF16) {
+        if (v == 8) launch_rotate<__bf16, 8>(a, mode, (unsigned)grid, st);
+        else if (v == 4) launch_rotate<__bf16, 4>(a, mode, (unsigned)grid, st);
+        else launch_rotate<__bf16, 1>(a, mode, (unsigned)grid, st);
+    } else {
+        if (v == 8) launch_rotate<_Float16, 8>(a, mode, (unsigned)grid, st);
+        else if (v == 4) launch_rotate<_Float16, 4>(a, mode, (unsigned)grid, st);
+        else launch_rotate<_Float16, 1>(a, mode, (unsigned)grid, st);
+    }
+    if (mode == kNormRotateBack) {
+        if (launched() != L3_OK) return L3_ERR_DEVICE;
+        hipLaunchKernelGGL(l3_weight_grad_kernel, dim3((unsigned)(2 * head_dim)), dim3(kRotateThreads), 0, st, partial, (int)grid,
+                           head_dim, q_weight_grad, k_weight_grad);
+    }
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t l3_patch_tokens_count(uint32_t width, uint32_t height, uint32_t side) {
+    if (!width || !height || !side || side > L3_MAX_PATCH_SIDE) return 0;
+    return (int64_t)(((uint64_t)width + side - 1) / side) * (int64_t)(((uint64_t)height + side - 1) / side);
+}
+
+l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n, uint32_t side,
+                                const float mean[3], const float stdv[3], l3_dtype dtype,
+                                void* d_tokens, int64_t tokens, int32_t* d_positions, int32_t* d_first,
+                                void* stream) {
+    if (!ctx || n < 0 || (n && !images) || !side || side > L3_MAX_PATCH_SIDE || !mean || !stdv || !known(dtype) || tokens < 0)
+        return L3_ERR_INVALID_ARG;
+    for (int c = 0; c < 3; ++c)
+        if (stdv[c] == 0.0f) return L3_ERR_INVALID_ARG;
+    int64_t total = 0;
+    bool too_many = false;
+    for (int i = 0; i < n; ++i) {
+        const l3_token_image& im = images[i];
+        if (!im.d_rgb || !im.width || !im.height || im.row_stride < 3 * (uint64_t)im.width) return L3_ERR_INVALID_ARG;
+        const int64_t count = l3_patch_tokens_count(im.width, im.height, side);
+        too_many = too_many || count >= (int64_t)1 << 31 || total + count >= (int64_t)1 << 31;
+        if (!too_many) total += count;
+    }
+    if (too_many) return L3_ERR_LIMIT;
+    if (tokens != total) return L3_ERR_INVALID_ARG;
+    if (n == 0) return L3_OK;
+    if (!d_tokens || !aligned(d_tokens, 16) || !aligned(d_positions, 4) || !aligned(d_first, 4)) return L3_ERR_INVALID_ARG;
+
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    TokenArgs a;
+    if (l3_normalized_values(mean, stdv, dtype, a.table) != L3_OK) return L3_ERR_INVALID_ARG;
+    a.tokens = (uint16_t*)d_tokens;
+    a.positions = d_positions;
+    a.first = d_first;
+    a.all_images = (uint32_t)n;
+    a.end_token = (uint32_t)total;
+    a.side = side;
+    a.per_strip = std::max(1u, kStripPixels / side);
+    const size_t lds = 768 * 2 + (size_t)a.per_strip * side * 3 * side;
+    uint32_t first = 0;
+    for (int i0 = 0; i0 < n; i0 += (int)kTokenImages) {
+        a.images = (uint32_t)std::min<int>((int)kTokenImages, n - i0);
+        a.image0 = (uint32_t)i0;
+        uint32_t blocks = 0;
+        for (uint32_t i = 0; i < a.images; ++i) {
+            const l3_token_image& im = images[i0 + (int)i];
+            const uint32_t cols = (uint32_t)(((uint64_t)im.width + side - 1) / side), rows = (uint32_t)(((uint64_t)im.height + side - 1) / side);
+            blocks += rows * ((cols + a.per_strip - 1) / a.per_strip);
+            a.image[i] = {im.d_rgb, im.row_stride, im.width, im.height, first, blocks};
+            first += cols * rows;
+        }
+        for (uint32_t i = a.images; i < kTokenImages; ++i) a.image[i] = {};
+        hipLaunchKernelGGL(l3_patch_tokens_kernel, dim3(blocks), dim3(kTokenThreads), lds, (hipStream_t)stream, a);
+        if (launched() != L3_OK) return L3_ERR_DEVICE;
+    }
+    return L3_OK;
+}
+
+l3_status l3_dropout(l3_ctx* ctx, const void* d_x, int64_t x_stride, const void* d_residual,
+                     int64_t residual_stride, void* d_y, int64_t y_stride, int64_t rows, int64_t cols,
+                     l3_dtype dtype, double p, uint64_t seed, uint64_t offset, const uint64_t* d_offset,
+                     void* stream) {
+    if (!ctx || !known(dtype) || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return L3_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return L3_OK;
+    if (!d_x || !d_y || x_stride < cols || y_stride < cols || (d_residual && residual_stride < cols)) return L3_ERR_INVALID_ARG;
+    if (!aligned(d_x, 2) || !aligned(d_y, 2) || !aligned(d_residual, 2) || !aligned(d_offset, 8)) return L3_ERR_INVALID_ARG;
+    if (cols >= ((int64_t)1 << 62) / rows) return L3_ERR_LIMIT;
+    DropoutArgs a = {d_x, d_residual, d_y, x_stride, residual_stride, y_stride, rows, cols, seed, offset, d_offset, 0.0f, 0u};
+    a.threshold = (uint32_t)(p * 65536.0 + 0.5);
+    a.scale = a.threshold < 65536u ? 65536.0f / (float)(65536u - a.threshold) : 0.0f;
+    /* one long row where the rows lie end to end */
+    if (rows == 1 || (x_stride == cols && y_stride == cols && (!d_residual || residual_stride == cols))) {
+        a.cols = rows * cols;
+        a.rows = 1;
+    }
+    const bool wide = a.rows == 1 && aligned(d_x, 16) && aligned(d_y, 16) && aligned(d_residual, 16);
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return L3_ERR_DEVICE;
+    return dtype == L3_BF16 ? launch_dropout<__bf16>(a, wide, (hipStream_t)stream) : launch_dropout<_Float16>(a, wide, (hipStream_t)stream);
+}
+
+l3_status l3_rotation_turns(int pairs, double base, double factor, double original_length, double slow, double fast, uint64_t* turns) {
+    if (!turns || pairs < 1 || pairs > L3_MAX_HEAD_DIM / 2 || !std::isfinite(base) || base <= 1.0 || !std::isfinite(factor) ||
+        factor < 1.0 || !std::isfinite(original_length) || original_length < 0.0 || !std::isfinite(slow) || !std::isfinite(fast) ||
+        slow >= fast)
+        return L3_ERR_INVALID_ARG;
+    const long double whole = 6.283185307179586476925286766559005768L;
+    for (int j = 0; j < pairs; ++j) {
+        long double f = powl((long double)base, -(long double)j / pairs);
+        if (factor > 1.0) {
+            long double keep = 0.0L;
+            if (original_length > 0.0) {
+                const long double t = (long double)original_length * f / whole;
+                keep = (t - (long double)slow) / ((long double)fast - (long double)slow);
+                keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
+            }
+            f *= keep + (1.0L - keep) / (long double)factor;
+        }
+        /* f <= 1 radian: below 0.16 of 2^64 */
+        turns[j] = (uint64_t)(f / whole * 18446744073709551616.0L + 0.5L);
+    }
+    return L3_OK;
+}
+
+l3_status l3_rotate(l3_ctx* ctx, const l3_rotation* rotation, int inverse, int64_t tokens, int head_dim,
+                    int q_heads, l3_heads q, l3_heads q_out, int k_heads, l3_heads k, l3_heads k_out,
+                    l3_dtype dtype, void* stream) {
+    const RotateSide side[2] = {{q_heads, q, q_out, {}, nullptr}, {k_heads, k, k_out, {}, nullptr}};
+    return run_rotate(ctx, rotation, inverse, 0.0f, tokens, head_dim, side, kRotate, dtype, nullptr, nullptr, nullptr, stream);
+}
+
+l3_status l3_norm_rotate(l3_ctx* ctx, const l3_rotation* rotation, float eps, int64_t tokens, int head_dim,
+                         int q_heads, l3_heads q, const float* d_q_weight, l3_heads q_out,
+                         int k_heads, l3_heads k, const float* d_k_weight, l3_heads k_out,
+                         l3_dtype dtype, void* stream) {
+    const RotateSide side[2] = {{q_heads, q, q_out, {}, d_q_weight}, {k_heads, k, k_out, {}, d_k_weight}};
+    return run_rotate(ctx, rotation, 0, eps, tokens, head_dim, side, kNormRotate, dtype, nullptr, nullptr, nullptr, stream);
+}
+
+l3_status l3_norm_rotate_backward(l3_ctx* ctx, const l3_rotation* rotation, float eps, int64_t tokens, int head_dim,
+                                  int q_heads, l3_heads q, const float* d_q_weight, l3_heads q_grad,
+                                  l3_heads q_back, float* d_q_weight_grad,
+                                  int k_heads, l3_heads k, const float* d_k_weight, l3_heads k_grad,
+                                  l3_heads k_back, float* d_k_weight_grad,
+                                  l3_dtype dtype, void* d_workspace, size_t workspace_bytes, void* stream) {
+    if (q_heads < 0 || k_heads < 0 || !d_workspace || !aligned(d_workspace, 16) || workspace_bytes < L3_NORM_ROTATE_WORKSPACE ||
+        (q_heads && !d_q_weight_grad) || (k_heads && !d_k_weight_grad))
+        return L3_ERR_INVALID_ARG;
+    if (q_heads + k_heads == 0) return L3_OK;
+    const RotateSide side[2] = {{q_heads, q, q_back, q_grad, d_q_weight}, {k_heads, k, k_back, k_grad, d_k_weight}};
+    return run_rotate(ctx, rotation, 0, eps, tokens, head_dim, side, kNormRotateBack, dtype, (float*)d_workspace, q_heads ? d_q_weight_grad : nullptr,
+                      k_heads ? d_k_weight_grad : nullptr, stream);
+}
+
+}  // extern "C"
