@@ -186,7 +186,7 @@ typedef struct {
  * held in 32 bits.  A key that no query of an image sees does not matter, whatever it holds; one that only some
  * see should be finite (its products with weights of 0 reach its neighbours in the causal order).
  * All tensors: 16-byte aligned, strides multiples of 8.
- * Errors: INVALID_ARG, LIMIT, DEVICE. */
+ * Errors: INVALID_ARG, LIMIT (also: token strides of 2^24 or more), DEVICE. */
 l3_status l3_attention(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
                        l3_heads out, float* d_lse, void* stream);
 

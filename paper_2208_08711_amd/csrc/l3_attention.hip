@@ -28,14 +28,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_const_void;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 constexpr int kThreads = 256;              /* 4 waves */
-
-/* What lanes read in place of rows and columns that the tensors do not have. */
-__device__ __attribute__((aligned(16))) uint32_t l3_zeros[4];
 
 __device__ __forceinline__ f32x16 mfma(HalfVec<__bf16, 8>::type a, HalfVec<__bf16, 8>::type b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -70,46 +66,105 @@ struct Tile {
         return kChunks == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : kChunks == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
     }
 
-    /* Rows row0 .. row0+ROWS-1 of a tensor, of which rows at or behind `end` and columns at or behind
-     * `dim` are taken as 0, straight from memory; THREADS threads take part, `t` is this one. */
-    template <typename T, int ROWS, int THREADS>
-    __device__ static __forceinline__ void fetch(uint8_t* lds, const T* base, int64_t stride, int row0, int end, int dim, int t) {
-        constexpr int kPlaces = ROWS * kChunks;
-        static_assert(kPlaces % 64 == 0 && (kPlaces % THREADS == 0 || kPlaces < THREADS), "whole waves, whole rounds");
+};
+
+/* Addresses in local memory are 32-bit numbers here: a lane's own, from which those of a tile's other
+ * steps differ by one exclusive or or a constant. */
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const lds_u8*)p; }
+
+/* A lane's place for operand rows: elements 16*step + 8*half .. +7 of row 32*block + (lane & 31) */
+template <int DB>
+__device__ __forceinline__ uint32_t row_place(int lane) {
+    const int r = lane & 31, half = lane >> 5;
+    return r * Tile<DB>::kPitch + (half ^ Tile<DB>::swizzle(r)) * 16;
+}
+template <typename T, int DB>
+__device__ __forceinline__ typename HalfVec<T, 8>::type read_row(uint32_t at, int block, int step) {
+    return __builtin_bit_cast(typename HalfVec<T, 8>::type, *(const lds_u32x4*)((at ^ (step * 32)) + block * 32 * Tile<DB>::kPitch));
+}
+
+/* A lane's places for operand columns: of column 32*db + (lane & 31) the rows row0 + 4*half + {0..3, 8..11},
+ * the order in which an accumulator's registers hold them.  row0 is a multiple of 16 and does not change
+ * the swizzle. */
+struct ColumnPlace {
+    uint32_t at[2];
+};
+template <int DB>
+__device__ __forceinline__ ColumnPlace column_place(int lane) {
+    ColumnPlace p;
 #pragma unroll
-        for (int i = 0; i < (kPlaces + THREADS - 1) / THREADS; ++i) {
-            const int place = i * THREADS + t;
-            if (kPlaces < THREADS && place >= kPlaces) break;
-            const int r = place / kChunks, c = (place % kChunks) ^ swizzle(r);
-            const bool there = row0 + r < end && c * 8 < dim;
-            const void* src = there ? (const void*)(base + (int64_t)(row0 + r) * stride + c * 8) : (const void*)l3_zeros;
+    for (int u = 0; u < 2; ++u) {
+        const int r = 8 * u + 4 * (lane >> 5) + ((lane & 15) >> 2), c = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+        p.at[u] = r * Tile<DB>::kPitch + (c ^ Tile<DB>::swizzle(r)) * 16 + (lane & 1) * 8;
+    }
+    return p;
+}
+template <typename T, int DB>
+__device__ __forceinline__ typename HalfVec<T, 8>::type read_columns(const ColumnPlace& p, int row0, int db) {
+    s16x4 part[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((p.at[u] ^ (db * 64)) + row0 * Tile<DB>::kPitch));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(typename HalfVec<T, 8>::type, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ ColumnPlace operator+(const ColumnPlace& p, uint32_t base) { return {{p.at[0] + base, p.at[1] + base}}; }
+
+/* Where a lane reads rows and columns of tiles */
+template <int DB>
+struct Reader {
+    uint32_t row;
+    ColumnPlace column;
+    __device__ __forceinline__ explicit Reader(int lane) : row(row_place<DB>(lane)), column(column_place<DB>(lane)) {}
+};
+
+/* Format word of an untyped buffer descriptor. */
+constexpr int kBufferFlags = 0x00020000;
+
+/* BYTES (4 or 16) a lane from byte `offset` of a buffer of `size` bytes at `base` to local memory: the wave's
+ * lanes one after the other from `lds` on; 0 for what lies outside.  base, size, lds: the wave's.
+ * (The descriptor's type exists in the device's compilation only.) */
+template <int BYTES>
+__device__ __forceinline__ void buffer_to_lds(uint32_t lds, const void* base, int32_t size, uint32_t offset) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, size, kBufferFlags);
+    if (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void*)(uintptr_t)lds, 16, offset, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void*)(uintptr_t)lds, 4, offset, 0, 0, 0);
+#endif
+}
+
+/* How THREADS threads bring ROWS rows of a tensor into a tile, 16 bytes a lane and round, straight from
+ * memory: through a buffer descriptor that ends with the last row that is there, so that rows behind it
+ * and columns behind the head come as 0 without a branch, and a lane keeps one offset (a few where a
+ * round is less than the 16 rows after which the swizzle repeats) for all tiles. */
+template <int DB, int ROWS, int THREADS>
+struct Fetch {
+    static constexpr int kChunks = Tile<DB>::kChunks, kRound = THREADS / kChunks;
+    static constexpr int kRounds = ROWS > kRound ? ROWS / kRound : 1, kOffsets = kRound >= 16 ? 1 : 16 / kRound;
+    static_assert(THREADS % 64 == 0 && (ROWS >= kRound ? ROWS % kRound == 0 : (ROWS * kChunks) % 64 == 0), "whole waves, whole rounds");
+    uint32_t offset[kOffsets];
+    int64_t stride;              /* bytes */
+    int32_t width;               /* bytes of a head */
+
+    __device__ __forceinline__ void set(int64_t row_stride, int dim, int t) {
+        stride = row_stride * 2;
+        width = dim * 2;
+#pragma unroll
+        for (int i = 0; i < kOffsets; ++i) {
+            const int r = t / kChunks, c = (t % kChunks) ^ Tile<DB>::swizzle(i * kRound + r);
+            offset[i] = c * 8 < dim ? (uint32_t)(r * stride) + c * 16 : 0xC0000000u;   /* (no descriptor is that long) */
+        }
+    }
+
+    /* Row 0 of the tile lies at `base`; `rows` rows are there (any number).  base, rows: the wave's. */
+    __device__ __forceinline__ void operator()(uint32_t lds, const void* base, int rows, int t) const {
+        if (ROWS < kRound && t >= ROWS * kChunks) return;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int left = rows - i * kRound;
+            const int32_t bytes = left > 0 ? (int32_t)(min(left, kRound) - 1) * (int32_t)stride + width : 0;
             const int first = i * THREADS + (t & ~63);  /* the wave's lanes write 16 bytes each from here on */
-            __builtin_amdgcn_global_load_lds((global_const_void*)src, (lds_void*)(lds + first * 16), 16, 0, 0);
+            buffer_to_lds<16>(lds + first * 16, (const uint8_t*)base + i * kRound * stride, bytes, offset[i % kOffsets]);
         }
-    }
-
-    /* Operand rows: elements 16*step + 8*half .. +7 of row `row` */
-    template <typename T>
-    __device__ static __forceinline__ typename HalfVec<T, 8>::type row(const uint8_t* lds, int row, int step, int half) {
-        const int c = (2 * step + half) ^ swizzle(row);
-        return __builtin_bit_cast(typename HalfVec<T, 8>::type, *(const u32x4*)(lds + row * kPitch + c * 16));
-    }
-
-    /* Operand columns: of column 32*db + (lane & 31) the rows row0 + 4*half + {0..3, 8..11}, the order in
-     * which an accumulator's registers hold them.  row0 is a multiple of 16. */
-    template <typename T>
-    __device__ static __forceinline__ typename HalfVec<T, 8>::type columns(const uint8_t* lds, int row0, int db, int lane) {
-        const int half = lane >> 5;
-        const int c = db * 4 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
-        s16x4 part[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int r = row0 + 8 * u + 4 * half + ((lane & 15) >> 2);
-            const uint8_t* p = lds + r * kPitch + (c ^ swizzle(r)) * 16 + (lane & 1) * 8;
-            part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-        }
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        return __builtin_bit_cast(typename HalfVec<T, 8>::type, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
@@ -177,10 +232,10 @@ __device__ Place find_tile(const Shape& s, int index, int rows, bool by_keys) {
         before += __shfl(upto, 63);
     }
     if (p.image >= 0) {
-        p.q0 = first_of(s.q_first, p.image, s.q_tokens);
-        p.n = max(0, first_of(s.q_first, p.image + 1, s.q_tokens) - p.q0);
-        p.k0 = first_of(s.kv_first, p.image, s.kv_tokens);
-        p.m = max(0, first_of(s.kv_first, p.image + 1, s.kv_tokens) - p.k0);
+        p.q0 = __builtin_amdgcn_readfirstlane(first_of(s.q_first, p.image, s.q_tokens));
+        p.n = __builtin_amdgcn_readfirstlane(max(0, first_of(s.q_first, p.image + 1, s.q_tokens) - p.q0));
+        p.k0 = __builtin_amdgcn_readfirstlane(first_of(s.kv_first, p.image, s.kv_tokens));
+        p.m = __builtin_amdgcn_readfirstlane(max(0, first_of(s.kv_first, p.image + 1, s.kv_tokens) - p.k0));
     }
     return p;
 }
@@ -193,13 +248,24 @@ __device__ __forceinline__ int seen_by(const Shape& s, const Place& p, int prefi
 }
 
 __device__ __forceinline__ int prefix_of(const Shape& s, const Place& p) {
-    return s.mask == L3_MASK_PREFIX ? min(max(s.prefix[p.image], 0), p.m) : 0;
+    return s.mask == L3_MASK_PREFIX ? __builtin_amdgcn_readfirstlane(min(max(s.prefix[p.image], 0), p.m)) : 0;
 }
 
-/* cap * tanh(x / cap) by the exponential: its error is a few 2^-24 of cap, not of the value. */
-__device__ __forceinline__ float tanh_of(float x) {
-    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+/* From a product of query and key to the exponent (base 2) of its weight, constants folded: cap * tanh(x / cap)
+ * is taken from the exponential, which is good to a few 2^-24 of cap. */
+struct Score {
+    float factor;        /* scale * log2 e */
+    float turn, high;    /* 2 log2 e * scale / cap; cap * log2 e */
+    float slope;         /* slope * log2 e */
+};
+
+__device__ __forceinline__ Score score_of(float scale, float cap, float slope) {
+    return {fmaxf(scale * kLog2e, 0x1p-126f) /* (-inf stays -inf) */, cap > 0.0f ? 2.0f * kLog2e * scale / cap : 0.0f, cap * kLog2e, slope * kLog2e};
+}
+
+/* tanh(scale * x / cap) */
+__device__ __forceinline__ float tanh_of(const Score& c, float x) {
+    return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * c.turn) + 1.0f), 1.0f);
 }
 
 /* ---- forward ------------------------------------------------------------------------------ */
@@ -220,44 +286,39 @@ struct Running {
 };
 
 /* One tile of KEYS keys against 32 queries.  key0: the tile's first key; seen: the keys that this
- * lane's query sees lie below it (whole: all of the tile does); place: the query's position. */
-template <typename T, int DB, int KEYS, bool CAP, bool SLOPES>
-__device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVec<T, 8>::type (&q)[2 * DB], const uint8_t* k_tile,
-                                         const uint8_t* v_tile, int key0, int seen, bool whole, int place, float scale, float cap,
-                                         float slope, int lane) {
+ * lane's query sees lie below it (not MASKED: all of the tile does); place: the query's position. */
+template <typename T, int DB, int KEYS, bool CAP, bool SLOPES, bool MASKED>
+__device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVec<T, 8>::type (&q)[2 * DB], const Reader<DB>& reader,
+                                         uint32_t k_tile, uint32_t v_tile, int key0, int seen, int place, const Score& c, int lane) {
     constexpr int KB = KEYS / 32;
     const int half = lane >> 5;
     f32x16 s[KB];
+    const uint32_t rows = reader.row + k_tile;
+    const ColumnPlace columns = reader.column + v_tile;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
         s[b] = f32x16{};
 #pragma unroll
-        for (int d = 0; d < 2 * DB; ++d) s[b] = mfma(Tile<DB>::template row<T>(k_tile, 32 * b + (lane & 31), d, half), q[d], s[b]);
+        for (int d = 0; d < 2 * DB; ++d) s[b] = mfma(read_row<T, DB>(rows, b, d), q[d], s[b]);
     }
-    const float factor = CAP || SLOPES ? kLog2e : fmaxf(scale * kLog2e, 0x1p-126f);   /* (-inf stays -inf) */
-    if (CAP || SLOPES) {
+    const float factor = CAP || SLOPES ? 1.0f : c.factor;
+    const float away = (float)(place - key0 - 4 * half);
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+    for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float v = s[b][r] * scale;
-                if (CAP) v = cap * tanh_of(v / cap);
-                if (SLOPES) v -= slope * fabsf((float)(place - (key0 + 32 * b + acc_row(r, half))));
-                s[b][r] = v;
-            }
-    }
-    if (!whole) {
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key0 + 32 * b + acc_row(r, half) >= seen) s[b][r] = -kInf;
-    }
+        for (int r = 0; r < 16; ++r) {
+            float v = s[b][r];
+            if (CAP) v = __builtin_fmaf(-2.0f * c.high, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v * c.turn) + 1.0f), c.high);
+            else if (SLOPES) v *= c.factor;
+            if (SLOPES) v = __builtin_fmaf(-c.slope, __builtin_fabsf(away - (float)(32 * b + acc_row(r, 0))), v);
+            if (MASKED && key0 + 32 * b + acc_row(r, half) >= seen) v = -kInf;
+            s[b][r] = v;
+        }
     float most = s[0][0];
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+        for (int r = 0; r < 16; ++r) most = __builtin_elementwise_maximum(most, s[b][r]);
     most = across_max(most) * factor;
     if (most != most) most = -kInf;
     /* The reference point moves only when a maximum outgrows it by 2^8: until then weights of up to 256
@@ -271,15 +332,15 @@ __device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVe
         run.top = top;
     }
     const float top = run.top > -kInf ? run.top : 0.0f;
-    float sum = 0.0f;
+    float sum[2] = {};
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], factor, -top));
-            sum += s[b][r];
+            s[b][r] = __builtin_amdgcn_exp2f(CAP || SLOPES ? s[b][r] - top : __builtin_fmaf(s[b][r], factor, -top));
+            sum[r & 1] += s[b][r];
         }
-    run.sum += sum;
+    run.sum += sum[0] + sum[1];
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -287,7 +348,7 @@ __device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVe
             const auto p = narrowed<T>(s[b], t);
 #pragma unroll
             for (int d = 0; d < DB; ++d)
-                run.out[d] = mfma(Tile<DB>::template columns<T>(v_tile, 32 * b + 16 * t, d, lane), p, run.out[d]);
+                run.out[d] = mfma(read_columns<T, DB>(columns, 32 * b + 16 * t, d), p, run.out[d]);
         }
 }
 
@@ -319,9 +380,11 @@ constexpr int kKeys = 64;                  /* of a tile */
 
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kThreads, 2) void l3_attention_kernel(ForwardArgs a) {
-    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kKeys * Tile<DB>::kPitch];
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kKeys * Tile<DB>::kPitch];
+    const uint32_t tiles_at = lds_address(tiles);
+    const auto tile = [&](int buffer, int which) { return tiles_at + (2 * buffer + which) * (uint32_t)(kKeys * Tile<DB>::kPitch); };
     const Shape& s = a.s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
     Place p = find_tile(s, index, kQueries, false);
     if (p.image < 0) return;
@@ -329,35 +392,40 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kernel(ForwardArgs a
     p.tile = (p.n + kQueries - 1) / kQueries - 1 - p.tile;
     const int prefix = prefix_of(s, p);
     const int row0 = p.tile * kQueries + wave * 32, row = row0 + (lane & 31);
-    const int last = min(p.tile * kQueries + kQueries, p.n) - 1;
-    const int all = seen_by(s, p, prefix, last);                 /* keys that any query of the workgroup sees */
-    const int wave_all = row0 < p.n ? seen_by(s, p, prefix, min(row0 + 31, p.n - 1)) : 0;
-    const int wave_whole = row0 < p.n ? seen_by(s, p, prefix, row0) : 0;
+    const int all = seen_by(s, p, prefix, min(p.tile * kQueries + kQueries, p.n) - 1);   /* keys that any query of the workgroup sees */
+    const int whole = seen_by(s, p, prefix, p.tile * kQueries);                            /* keys that all of them see */
     const int seen = row < p.n ? seen_by(s, p, prefix, row) : 0;
-    const float slope = SLOPES ? s.slopes[head] : 0.0f;
+    const Score score = score_of(s.scale, s.cap, SLOPES ? s.slopes[head] : 0.0f);
 
     typename HalfVec<T, 8>::type q[2 * DB];
     load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)(p.q0 + row) * a.q.token + (int64_t)head * a.q.head, row < p.n, s.head_dim, half);
     const T* const k = (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head;
     const T* const v = (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head;
+    Fetch<DB, kKeys, kThreads> fetch_k, fetch_v;
+    fetch_k.set(a.k.token, s.head_dim, threadIdx.x);
+    fetch_v.set(a.v.token, s.head_dim, threadIdx.x);
+    const Reader<DB> reader(lane);
     Running<DB> run;
     run.start();
-    const int steps = (all + kKeys - 1) / kKeys;
-    if (steps > 0) {
-        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][0], k, a.k.token, 0, p.m, s.head_dim, threadIdx.x);
-        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][1], v, a.v.token, 0, p.m, s.head_dim, threadIdx.x);
-    }
-    for (int i = 0; i < steps; ++i) {
+    const int steps = (all + kKeys - 1) / kKeys, plain = whole / kKeys;
+    const auto fetch = [&](int i) {
+        if (i >= steps) return;
+        fetch_k(tile(i & 1, 0), k + (int64_t)i * kKeys * a.k.token, p.m - i * kKeys, threadIdx.x);
+        fetch_v(tile(i & 1, 1), v + (int64_t)i * kKeys * a.v.token, p.m - i * kKeys, threadIdx.x);
+    };
+    fetch(0);
+    int i = 0;
+    for (; i < plain; ++i) {
         fetched();
         __syncthreads();
-        const int key0 = i * kKeys;
-        if (i + 1 < steps) {
-            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][0], k, a.k.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
-            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][1], v, a.v.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
-        }
-        if (key0 < wave_all)
-            one_tile<T, DB, kKeys, CAP, SLOPES>(run, q, tiles[i & 1][0], tiles[i & 1][1], key0, seen, key0 + kKeys <= wave_whole,
-                                                row + p.m - p.n, s.scale, s.cap, slope, lane);
+        fetch(i + 1);
+        one_tile<T, DB, kKeys, CAP, SLOPES, false>(run, q, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, row + p.m - p.n, score, lane);
+    }
+    for (; i < steps; ++i) {
+        fetched();
+        __syncthreads();
+        fetch(i + 1);
+        one_tile<T, DB, kKeys, CAP, SLOPES, true>(run, q, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, row + p.m - p.n, score, lane);
     }
     if (row >= p.n) return;
     const float sum = across_sum(run.sum);
@@ -383,12 +451,15 @@ struct BackwardArgs {
     Shape s;
     Heads q, k, v, out, out_grad, q_grad, k_grad, v_grad;
     const float* lse;
-    float* delta;                          /* [q_heads][q_tokens]: dot(out, its gradient) */
+    float* stats;                          /* [q_heads][q_tokens][2]: lse in log2 and delta = dot(out, its gradient) */
+    float* partial;                        /* [2][splits][kv_tokens][kv_heads][head_dim], where splits > 1 */
+    int32_t splits;                        /* workgroups that share a tile of keys, each with some of the query heads */
 };
 
-/* delta: 16 lanes a head, 8 elements each */
+/* lse to log2 (+inf, so that all weights are 0, for a query that sees nothing); delta: 16 lanes a
+ * head, 8 elements each */
 template <typename T>
-__global__ __launch_bounds__(kThreads) void l3_attention_delta_kernel(BackwardArgs a) {
+__global__ __launch_bounds__(kThreads) void l3_attention_stats_kernel(BackwardArgs a) {
     const Shape& s = a.s;
     const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 16;
     const int64_t token = at / s.q_heads;
@@ -403,38 +474,81 @@ __global__ __launch_bounds__(kThreads) void l3_attention_delta_kernel(BackwardAr
         for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], g[i], sum);
     }
     for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d);
-    if (there && (threadIdx.x & 15) == 0) a.delta[(int64_t)head * s.q_tokens + token] = sum;
-}
-
-/* The weight of a score (raw product s) and what its gradient is multiplied with on the way to
- * the raw product, but for the scale. */
-template <bool CAP, bool SLOPES>
-__device__ __forceinline__ float weight_of(float s, float scale, float cap, float slope, int distance, float lse2, float& steep) {
-    steep = 1.0f;
-    if (!CAP && !SLOPES) return __builtin_amdgcn_exp2f(__builtin_fmaf(s, scale * kLog2e, -lse2));
-    float v = s * scale;
-    if (CAP) {
-        const float t = tanh_of(v / cap);
-        v = cap * t;
-        steep = 1.0f - t * t;
+    if (there && (threadIdx.x & 15) == 0) {
+        const int64_t to = (int64_t)head * s.q_tokens + token;
+        const float lse = a.lse[to];
+        a.stats[2 * to] = lse == -kInf ? kInf : lse * kLog2e;
+        a.stats[2 * to + 1] = sum;
     }
-    if (SLOPES) v -= slope * fabsf((float)distance);
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(v, kLog2e, -lse2));
 }
 
-/* lse in log2; +inf (all weights 0) for a query that sees nothing or is not there */
-__device__ __forceinline__ float lse2_of(const float* lse, int64_t at, bool there) {
-    if (!there) return kInf;
-    const float v = lse[at];
-    return v > -kInf ? v * kLog2e : (v == -kInf ? kInf : v);
+/* The weight of a raw product s, and what its gradient is multiplied with on the way to the raw product,
+ * but for the scale.  away: distance of query and key. */
+template <bool CAP, bool SLOPES>
+__device__ __forceinline__ float weight_of(const Score& c, float s, float away, float lse2, float& steep) {
+    steep = 1.0f;
+    if (!CAP && !SLOPES) return __builtin_amdgcn_exp2f(__builtin_fmaf(s, c.factor, -lse2));
+    float v;
+    if (CAP) {
+        const float t = tanh_of(c, s);
+        v = __builtin_fmaf(t, c.high, -lse2);
+        steep = __builtin_fmaf(-t, t, 1.0f);
+    } else {
+        v = __builtin_fmaf(s, c.factor, -lse2);
+    }
+    if (SLOPES) v = __builtin_fmaf(-c.slope, __builtin_fabsf(away), v);
+    return __builtin_amdgcn_exp2f(v);
 }
 
-/* Gradients of the queries: as the forward, 32 queries a wave, over the keys. */
+/* One tile of keys on the way to the gradients of 32 queries; DELTA: only the sum of the weights times the
+ * gradients of the weights, into delta. */
+template <typename T, int DB, bool CAP, bool SLOPES, bool MASKED, bool DELTA>
+__device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, const typename HalfVec<T, 8>::type (&q)[2 * DB],
+                                            const typename HalfVec<T, 8>::type (&g)[2 * DB], const Reader<DB>& reader, uint32_t k_tile, uint32_t v_tile,
+                                            int key0, int seen, int place, float lse2, const Score& c, int lane) {
+    const int half = lane >> 5;
+    const float away = (float)(place - key0 - 4 * half);
+    const uint32_t k_rows = reader.row + k_tile, v_rows = reader.row + v_tile;
+    const ColumnPlace columns = reader.column + k_tile;
+#pragma unroll
+    for (int b = 0; b < kKeys / 32; ++b) {
+        f32x16 x = {}, dp = {};
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d) {
+            x = mfma(read_row<T, DB>(k_rows, b, d), q[d], x);
+            dp = mfma(read_row<T, DB>(v_rows, b, d), g[d], dp);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float steep;
+            const float w = weight_of<CAP, SLOPES>(c, x[r], away - (float)(32 * b + acc_row(r, 0)), lse2, steep);
+            const bool hidden = MASKED && key0 + 32 * b + acc_row(r, half) >= seen;
+            if (DELTA) delta += hidden ? 0.0f : w * dp[r];
+            else x[r] = hidden ? 0.0f : (CAP ? w * steep : w) * (dp[r] - delta);
+        }
+        if (DELTA) continue;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const auto ds = narrowed<T>(x, t);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) grad[d] = mfma(read_columns<T, DB>(columns, 32 * b + 16 * t, d), ds, grad[d]);
+        }
+    }
+}
+
+/* Gradients of the queries: as the forward, 32 queries a wave, over the keys.  Where the keys are few (two
+ * tiles at most), delta is summed up from weights and products here rather than taken from the narrowed
+ * results, whose rounding weighs most there (in fp16, images of 5 tokens: gradients off by 3e-4 instead of 6e-4,
+ * of 500 tokens 2.9e-4 instead of 3.0e-4); for the first tokens under a causal mask too. */
+constexpr int kExactSteps = 2;
+
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(BackwardArgs a) {
-    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kKeys * Tile<DB>::kPitch];
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kKeys * Tile<DB>::kPitch];
+    const uint32_t tiles_at = lds_address(tiles);
+    const auto tile = [&](int buffer, int which) { return tiles_at + (2 * buffer + which) * (uint32_t)(kKeys * Tile<DB>::kPitch); };
     const Shape& s = a.s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
     Place p = find_tile(s, index, kQueries, false);
     if (p.image < 0) return;
@@ -442,62 +556,58 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
     const int prefix = prefix_of(s, p);
     const int row0 = p.tile * kQueries + wave * 32, row = row0 + (lane & 31);
     const int all = seen_by(s, p, prefix, min(p.tile * kQueries + kQueries, p.n) - 1);
-    const int wave_all = row0 < p.n ? seen_by(s, p, prefix, min(row0 + 31, p.n - 1)) : 0;
-    const int wave_whole = row0 < p.n ? seen_by(s, p, prefix, row0) : 0;
+    const int whole = seen_by(s, p, prefix, p.tile * kQueries);
     const int seen = row < p.n ? seen_by(s, p, prefix, row) : 0;
-    const float slope = SLOPES ? s.slopes[head] : 0.0f;
     const int place = row + p.m - p.n;
+    const Score score = score_of(s.scale, s.cap, SLOPES ? s.slopes[head] : 0.0f);
 
     typename HalfVec<T, 8>::type q[2 * DB], g[2 * DB];
     load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)(p.q0 + row) * a.q.token + (int64_t)head * a.q.head, row < p.n, s.head_dim, half);
     load_operand<T, DB>(g, (const T*)a.out_grad.d + (int64_t)(p.q0 + row) * a.out_grad.token + (int64_t)head * a.out_grad.head, row < p.n,
                         s.head_dim, half);
-    const int64_t at = (int64_t)head * s.q_tokens + p.q0 + row;
-    const float lse2 = lse2_of(a.lse, at, row < p.n), delta = row < p.n ? a.delta[at] : 0.0f;
+    float* const stats = a.stats + 2 * ((int64_t)head * s.q_tokens + p.q0 + row);
+    const float lse2 = row < p.n ? stats[0] : kInf;
+    float delta = row < p.n ? stats[1] : 0.0f;
     const T* const k = (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head;
     const T* const v = (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head;
+    Fetch<DB, kKeys, kThreads> fetch_k, fetch_v;
+    fetch_k.set(a.k.token, s.head_dim, threadIdx.x);
+    fetch_v.set(a.v.token, s.head_dim, threadIdx.x);
+    const Reader<DB> reader(lane);
     f32x16 grad[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) grad[d] = f32x16{};
-    const int steps = (all + kKeys - 1) / kKeys;
-    if (steps > 0) {
-        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][0], k, a.k.token, 0, p.m, s.head_dim, threadIdx.x);
-        Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[0][1], v, a.v.token, 0, p.m, s.head_dim, threadIdx.x);
-    }
-    for (int i = 0; i < steps; ++i) {
+    const int steps = (all + kKeys - 1) / kKeys, plain = whole / kKeys;
+    const auto fetch = [&](int i) {
+        if (i >= steps) return;
+        fetch_k(tile(i & 1, 0), k + (int64_t)i * kKeys * a.k.token, p.m - i * kKeys, threadIdx.x);
+        fetch_v(tile(i & 1, 1), v + (int64_t)i * kKeys * a.v.token, p.m - i * kKeys, threadIdx.x);
+    };
+    fetch(0);
+    if (steps <= kExactSteps) {
+        fetch(1);
         fetched();
         __syncthreads();
-        const int key0 = i * kKeys;
-        if (i + 1 < steps) {
-            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][0], k, a.k.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
-            Tile<DB>::template fetch<T, kKeys, kThreads>(tiles[(i + 1) & 1][1], v, a.v.token, key0 + kKeys, p.m, s.head_dim, threadIdx.x);
+        float sum = 0.0f;
+        for (int i = 0; i < steps; ++i)
+            q_grad_tile<T, DB, CAP, SLOPES, true, true>(grad, sum, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
+        delta = across_sum(sum);
+        if (row < p.n && half == 0) stats[1] = delta;
+        for (int i = 0; i < steps; ++i)
+            q_grad_tile<T, DB, CAP, SLOPES, true, false>(grad, delta, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
+    } else {
+        int i = 0;
+        for (; i < plain; ++i) {
+            fetched();
+            __syncthreads();
+            fetch(i + 1);
+            q_grad_tile<T, DB, CAP, SLOPES, false, false>(grad, delta, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
         }
-        if (key0 >= wave_all) continue;
-        const uint8_t* const k_tile = tiles[i & 1][0];
-        const uint8_t* const v_tile = tiles[i & 1][1];
-        const bool whole = key0 + kKeys <= wave_whole;
-#pragma unroll
-        for (int b = 0; b < kKeys / 32; ++b) {
-            f32x16 x = {}, dp = {};
-#pragma unroll
-            for (int d = 0; d < 2 * DB; ++d) {
-                x = mfma(Tile<DB>::template row<T>(k_tile, 32 * b + (lane & 31), d, half), q[d], x);
-                dp = mfma(Tile<DB>::template row<T>(v_tile, 32 * b + (lane & 31), d, half), g[d], dp);
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = key0 + 32 * b + acc_row(r, half);
-                float steep;
-                const float w = weight_of<CAP, SLOPES>(x[r], s.scale, s.cap, slope, place - key, lse2, steep);
-                const float ds = w * (dp[r] - delta) * steep;
-                x[r] = whole || key < seen ? ds : 0.0f;
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const auto ds = narrowed<T>(x, t);
-#pragma unroll
-                for (int d = 0; d < DB; ++d) grad[d] = mfma(Tile<DB>::template columns<T>(k_tile, 32 * b + 16 * t, d, lane), ds, grad[d]);
-            }
+        for (; i < steps; ++i) {
+            fetched();
+            __syncthreads();
+            fetch(i + 1);
+            q_grad_tile<T, DB, CAP, SLOPES, true, false>(grad, delta, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
         }
     }
     if (row >= p.n) return;
@@ -518,88 +628,121 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
 constexpr int kBackKeys = 128;             /* of a workgroup: 32 a wave */
 constexpr int kBackQueries = 32;           /* of a tile */
 
+/* One tile of queries against the 32 keys of a wave.  stats: lse and delta of the tile's queries. */
+template <typename T, int DB, bool CAP, bool SLOPES, bool MASKED>
+__device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB], const typename HalfVec<T, 8>::type (&k)[2 * DB],
+                                             const typename HalfVec<T, 8>::type (&v)[2 * DB], const Reader<DB>& reader, uint32_t q_tile, uint32_t g_tile,
+                                             const float* stats, const Shape& s, const Place& p, int prefix, int row0, int key, const Score& c, int lane) {
+    const int half = lane >> 5;
+    f32x16 x = {}, dp = {};
+#pragma unroll
+    for (int d = 0; d < 2 * DB; ++d) {
+        x = mfma(read_row<T, DB>(reader.row + q_tile, 0, d), k[d], x);
+        dp = mfma(read_row<T, DB>(reader.row + g_tile, 0, d), v[d], dp);
+    }
+    const float away = (float)(row0 + p.m - p.n - key + 4 * half);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const float2 stat = *(const float2*)(stats + 2 * acc_row(r, half));
+        float steep;
+        float w = weight_of<CAP, SLOPES>(c, x[r], away + (float)acc_row(r, 0), stat.x, steep);
+        if (MASKED && key >= seen_by(s, p, prefix, row0 + acc_row(r, half))) w = 0.0f;
+        const float ds = (CAP ? w * steep : w) * (dp[r] - stat.y);
+        dp[r] = MASKED && w == 0.0f ? 0.0f : ds;
+        x[r] = w;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const auto w = narrowed<T>(x, t), ds = narrowed<T>(dp, t);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            dv[d] = mfma(read_columns<T, DB>(reader.column + g_tile, 16 * t, d), w, dv[d]);
+            dk[d] = mfma(read_columns<T, DB>(reader.column + q_tile, 16 * t, d), ds, dk[d]);
+        }
+    }
+}
+
 /* Gradients of keys and values: 32 keys a wave (one a lane), over the queries of all heads that share
- * them.  S = Q K^T gives a lane 16 queries of its key, and P and dS are second operands of
- * dV^T = dO^T P and dK^T = Q^T dS as they are. */
+ * them (or, split, of some of these).  S = Q K^T gives a lane 16 queries of its key, and P and dS are second
+ * operands of dV^T = dO^T P and dK^T = Q^T dS as they are. */
 template <typename T, int DB, bool CAP, bool SLOPES>
-__global__ __launch_bounds__(kThreads, 1) void l3_attention_kv_grad_kernel(BackwardArgs a) {
-    __shared__ __attribute__((aligned(256))) uint8_t tiles[2][2][kBackQueries * Tile<DB>::kPitch];
-    __shared__ float stats[2][2][kBackQueries];
+__global__ __launch_bounds__(kThreads, DB >= 3 ? 1 : 2) void l3_attention_kv_grad_kernel(BackwardArgs a) {
+    __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kBackQueries * Tile<DB>::kPitch];
+    const uint32_t tiles_at = lds_address(tiles);
+    const auto tile = [&](int buffer, int which) { return tiles_at + (2 * buffer + which) * (uint32_t)(kBackQueries * Tile<DB>::kPitch); };
+    __shared__ __attribute__((aligned(16))) float stats[2][kBackQueries * 2];
     const Shape& s = a.s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const int index = blockIdx.x / s.kv_heads, kv_head = blockIdx.x - index * s.kv_heads;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    int at = blockIdx.x;
+    const int split = at % a.splits;
+    at /= a.splits;
+    const int index = at / s.kv_heads, kv_head = at - index * s.kv_heads;
     const Place p = find_tile(s, index, kBackKeys, true);
     if (p.image < 0) return;
     const int prefix = prefix_of(s, p);
     const int tile0 = p.tile * kBackKeys;
-    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31);
+    const int key = tile0 + wave * 32 + (lane & 31);
+    const int heads = s.group / a.splits, head0 = kv_head * s.group + split * heads;
 
     typename HalfVec<T, 8>::type k[2 * DB], v[2 * DB];
     load_operand<T, DB>(k, (const T*)a.k.d + (int64_t)(p.k0 + key) * a.k.token + (int64_t)kv_head * a.k.head, key < p.m, s.head_dim, half);
     load_operand<T, DB>(v, (const T*)a.v.d + (int64_t)(p.k0 + key) * a.v.token + (int64_t)kv_head * a.v.head, key < p.m, s.head_dim, half);
+    Fetch<DB, kBackQueries, kThreads> fetch_q, fetch_g;
+    fetch_q.set(a.q.token, s.head_dim, threadIdx.x);
+    fetch_g.set(a.out_grad.token, s.head_dim, threadIdx.x);
+    const Reader<DB> reader(lane);
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
 
-    /* queries from here on see keys of the workgroup */
-    const int shift = p.m - p.n;
+    /* queries from `begin` on see keys of the workgroup; from the tile at `plain` on they see all of them */
     int begin = 0;
-    if (s.mask != L3_MASK_DOCUMENT && tile0 >= prefix) begin = min(max(tile0 - shift, 0), p.n) / kBackQueries * kBackQueries;
-    const int per_head = (p.n - begin + kBackQueries - 1) / kBackQueries, steps = per_head * s.group;
-    const auto fetch = [&](int i, int buffer) {
-        const int of = i / per_head, head = kv_head * s.group + of, row0 = begin + (i - of * per_head) * kBackQueries;
-        Tile<DB>::template fetch<T, kBackQueries, kThreads>(
-            tiles[buffer][0], (const T*)a.q.d + (int64_t)p.q0 * a.q.token + (int64_t)head * a.q.head, a.q.token, row0, p.n, s.head_dim, threadIdx.x);
-        Tile<DB>::template fetch<T, kBackQueries, kThreads>(
-            tiles[buffer][1], (const T*)a.out_grad.d + (int64_t)p.q0 * a.out_grad.token + (int64_t)head * a.out_grad.head, a.out_grad.token, row0,
-            p.n, s.head_dim, threadIdx.x);
-        if (threadIdx.x < kBackQueries) {
-            const int row = row0 + (int)threadIdx.x;
-            const int64_t at = (int64_t)head * s.q_tokens + p.q0 + row;
-            stats[buffer][0][threadIdx.x] = lse2_of(a.lse, at, row < p.n);
-            stats[buffer][1][threadIdx.x] = row < p.n ? a.delta[at] : 0.0f;
+    if (s.mask != L3_MASK_DOCUMENT && tile0 >= prefix) begin = min(max(tile0 - (p.m - p.n), 0), p.n) / kBackQueries * kBackQueries;
+    const int steps = (p.n - begin + kBackQueries - 1) / kBackQueries, last = min(tile0 + kBackKeys, p.m);
+    int masked = 0;
+    while (masked < steps && seen_by(s, p, prefix, begin + masked * kBackQueries) < last) ++masked;
+    const auto fetch = [&](int h, int i, int buffer) {
+        if (i >= steps) {
+            i = 0;
+            ++h;
+        }
+        if (h >= heads || steps == 0) return;
+        const int row0 = begin + i * kBackQueries;
+        const int64_t row = (int64_t)p.q0 + row0;
+        fetch_q(tile(buffer, 0), (const T*)a.q.d + row * a.q.token + (int64_t)(head0 + h) * a.q.head, p.n - row0, threadIdx.x);
+        fetch_g(tile(buffer, 1), (const T*)a.out_grad.d + row * a.out_grad.token + (int64_t)(head0 + h) * a.out_grad.head, p.n - row0, threadIdx.x);
+        if (threadIdx.x < 64) {
+            /* queries that are not there come as 0: so do their rows, and then all their products */
+            buffer_to_lds<4>(lds_address(&stats[buffer][0]), a.stats + 2 * ((int64_t)(head0 + h) * s.q_tokens + row),
+                             min(p.n - row0, kBackQueries) * 8, threadIdx.x * 4);
         }
     };
-    if (steps > 0) fetch(0, 0);
-    for (int i = 0; i < steps; ++i) {
-        fetched();
-        __syncthreads();
-        if (i + 1 < steps) fetch(i + 1, (i + 1) & 1);
-        const int of = i / per_head, row0 = begin + (i - of * per_head) * kBackQueries;
-        const float slope = SLOPES ? s.slopes[kv_head * s.group + of] : 0.0f;
-        /* does every query of the tile see every key of the wave?  any? */
-        const bool whole = s.mask == L3_MASK_DOCUMENT || key0 + 31 < seen_by(s, p, prefix, row0);
-        if (s.mask != L3_MASK_DOCUMENT && key0 >= seen_by(s, p, prefix, min(row0 + kBackQueries, p.n) - 1)) continue;
-        const uint8_t* const q_tile = tiles[i & 1][0];
-        const uint8_t* const g_tile = tiles[i & 1][1];
-        f32x16 x = {}, dp = {};
-#pragma unroll
-        for (int d = 0; d < 2 * DB; ++d) {
-            x = mfma(Tile<DB>::template row<T>(q_tile, lane & 31, d, half), k[d], x);
-            dp = mfma(Tile<DB>::template row<T>(g_tile, lane & 31, d, half), v[d], dp);
+    fetch(0, 0, 0);
+    int buffer = 0;
+    for (int h = 0; h < heads; ++h) {
+        const Score score = score_of(s.scale, s.cap, SLOPES ? s.slopes[head0 + h] : 0.0f);
+        int i = 0;
+        for (; i < masked; ++i, buffer ^= 1) {
+            fetched();
+            __syncthreads();
+            fetch(h, i + 1, buffer ^ 1);
+            kv_grad_tile<T, DB, CAP, SLOPES, true>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), stats[buffer], s, p, prefix,
+                                                   begin + i * kBackQueries, key, score, lane);
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int in = acc_row(r, half), row = row0 + in;
-            float steep;
-            float w = weight_of<CAP, SLOPES>(x[r], s.scale, s.cap, slope, row + shift - key, stats[i & 1][0][in], steep);
-            if (!whole && key >= seen_by(s, p, prefix, row)) w = 0.0f;
-            dp[r] = w > 0.0f || w != w ? w * (dp[r] - stats[i & 1][1][in]) * steep : 0.0f;
-            x[r] = w;
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const auto w = narrowed<T>(x, t), ds = narrowed<T>(dp, t);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                dv[d] = mfma(Tile<DB>::template columns<T>(g_tile, 16 * t, d, lane), w, dv[d]);
-                dk[d] = mfma(Tile<DB>::template columns<T>(q_tile, 16 * t, d, lane), ds, dk[d]);
-            }
+        for (; i < steps; ++i, buffer ^= 1) {
+            fetched();
+            __syncthreads();
+            fetch(h, i + 1, buffer ^ 1);
+            kv_grad_tile<T, DB, CAP, SLOPES, false>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), stats[buffer], s, p, prefix,
+                                                    begin + i * kBackQueries, key, score, lane);
         }
     }
     if (key >= p.m) return;
-    T* const k_out = (T*)const_cast<void*>(a.k_grad.d) + (int64_t)(p.k0 + key) * a.k_grad.token + (int64_t)kv_head * a.k_grad.head;
-    T* const v_out = (T*)const_cast<void*>(a.v_grad.d) + (int64_t)(p.k0 + key) * a.v_grad.token + (int64_t)kv_head * a.v_grad.head;
+    const int64_t row = p.k0 + key;
+    T* const k_out = (T*)const_cast<void*>(a.k_grad.d) + row * a.k_grad.token + (int64_t)kv_head * a.k_grad.head;
+    T* const v_out = (T*)const_cast<void*>(a.v_grad.d) + row * a.v_grad.token + (int64_t)kv_head * a.v_grad.head;
+    const int64_t plane = (int64_t)a.splits * s.kv_tokens * s.kv_heads * s.head_dim;
+    float* const part = a.partial + (((int64_t)split * s.kv_tokens + row) * s.kv_heads + kv_head) * s.head_dim;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -612,9 +755,40 @@ __global__ __launch_bounds__(kThreads, 1) void l3_attention_kv_grad_kernel(Backw
                 y[i] = dk[d][4 * e + i] * s.scale;
                 z[i] = dv[d][4 * e + i];
             }
-            store_narrow<T, 4>(k_out + c, y);
-            store_narrow<T, 4>(v_out + c, z);
+            if (a.splits > 1) {
+                *(float4*)(part + c) = float4{y[0], y[1], y[2], y[3]};
+                *(float4*)(part + plane + c) = float4{z[0], z[1], z[2], z[3]};
+            } else {
+                store_narrow<T, 4>(k_out + c, y);
+                store_narrow<T, 4>(v_out + c, z);
+            }
         }
+}
+
+/* The splits' sums joined, in order; 4 elements a thread, of keys and values. */
+template <typename T>
+__global__ __launch_bounds__(kThreads) void l3_attention_kv_join_kernel(BackwardArgs a) {
+    const Shape& s = a.s;
+    const int64_t plane = (int64_t)s.kv_tokens * s.kv_heads * s.head_dim;
+    const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (at >= plane) return;
+    const int64_t row = at / (s.kv_heads * s.head_dim);
+    if (row >= first_of(s.kv_first, s.images, s.kv_tokens)) return;
+    const int rest = (int)(at - row * (s.kv_heads * s.head_dim)), head = rest / s.head_dim, c = rest - head * s.head_dim;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const float* from = a.partial + which * a.splits * plane + at;
+        float x[4] = {};
+        for (int i = 0; i < a.splits; ++i, from += plane) {
+            const float4 v = *(const float4*)from;
+            x[0] += v.x;
+            x[1] += v.y;
+            x[2] += v.z;
+            x[3] += v.w;
+        }
+        const Heads& to = which ? a.v_grad : a.k_grad;
+        store_narrow<T, 4>((T*)const_cast<void*>(to.d) + row * to.token + (int64_t)head * to.head + c, x);
+    }
 }
 
 /* ---- single tokens ------------------------------------------------------------------------- */
@@ -640,14 +814,14 @@ template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(StepArgs a) {
     constexpr int kTile = kStepKeys * Tile<DB>::kPitch;
     extern __shared__ __attribute__((aligned(256))) uint8_t step_lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     int at = blockIdx.x;
     const int chunk = at % a.chunks;
     at /= a.chunks;
     const int of = at % a.blocks_of_heads;
     at /= a.blocks_of_heads;
     const int kv_head = at % a.kv_heads, sequence = at / a.kv_heads;
-    const int length = min(max(a.lengths[sequence], 0), a.max_length);
+    const int length = __builtin_amdgcn_readfirstlane(min(max(a.lengths[sequence], 0), a.max_length));
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, length);
     const int in_group = of * 32 + (lane & 31), head = kv_head * a.group + in_group;
     const bool there = in_group < a.group;
@@ -655,26 +829,34 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
 
     typename HalfVec<T, 8>::type q[2 * DB];
     load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)sequence * a.q.token + (int64_t)head * a.q.head, there, a.head_dim, half);
-    const float slope = SLOPES && there ? a.slopes[head] : 0.0f;
+    const Score score = score_of(a.scale, a.cap, SLOPES && there ? a.slopes[head] : 0.0f);
     const T* const k = (const T*)a.k.d + (int64_t)sequence * a.k_sequence + (int64_t)kv_head * a.k.head;
     const T* const v = (const T*)a.v.d + (int64_t)sequence * a.v_sequence + (int64_t)kv_head * a.v.head;
-    uint8_t* const own = step_lds + wave * 4 * kTile;              /* 2 stages of keys and values */
+    const uint32_t own = lds_address(step_lds) + wave * 4 * kTile;              /* 2 stages of keys and values */
+    const Reader<DB> reader(lane);
     Running<DB> run;
     run.start();
     const int first = begin + wave * kStepKeys;
+    Fetch<DB, kStepKeys, 64> fetch_k, fetch_v;
+    fetch_k.set(a.k.token, a.head_dim, lane);
+    fetch_v.set(a.v.token, a.head_dim, lane);
     const auto fetch = [&](int key0, int stage) {
-        Tile<DB>::template fetch<T, kStepKeys, 64>(own + stage * 2 * kTile, k, a.k.token, key0, end, a.head_dim, lane);
-        Tile<DB>::template fetch<T, kStepKeys, 64>(own + stage * 2 * kTile + kTile, v, a.v.token, key0, end, a.head_dim, lane);
+        if (key0 >= end) return;
+        fetch_k(own + stage * 2 * kTile, k + key0 * a.k.token, end - key0, lane);
+        fetch_v(own + stage * 2 * kTile + kTile, v + key0 * a.v.token, end - key0, lane);
     };
-    if (first < end) fetch(first, 0);
-    int stage = 0;
-    for (int key0 = first; key0 < end; key0 += kStepWaves * kStepKeys, stage ^= 1) {
+    fetch(first, 0);
+    int stage = 0, key0 = first;
+    for (; key0 + kStepKeys <= end; key0 += kStepWaves * kStepKeys, stage ^= 1) {
         fetched();
-        if (key0 + kStepWaves * kStepKeys < end) fetch(key0 + kStepWaves * kStepKeys, stage ^ 1);
-        one_tile<T, DB, kStepKeys, CAP, SLOPES>(run, q, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, key0 + kStepKeys <= end,
-                                                length - 1, a.scale, a.cap, slope, lane);
+        fetch(key0 + kStepWaves * kStepKeys, stage ^ 1);
+        one_tile<T, DB, kStepKeys, CAP, SLOPES, false>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, length - 1, score, lane);
         /* this wave's reads of the tile have come back before the next fetch into it is sent */
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    if (key0 < end) {
+        fetched();
+        one_tile<T, DB, kStepKeys, CAP, SLOPES, true>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, length - 1, score, lane);
     }
 
     /* join the waves: reference point, sum and products of each through local memory */
@@ -752,6 +934,10 @@ bool good_numbers(int head_dim, int q_heads, int kv_heads, float scale, float ca
            q_heads % kv_heads == 0 && scale >= 0.0f && std::isfinite(scale) && cap >= 0.0f && std::isfinite(cap);
 }
 
+/* Rows of a tile are reached by 32-bit offsets. */
+constexpr int64_t kMostStride = (int64_t)1 << 24;
+bool far_apart(const l3_heads& h) { return h.token_stride >= kMostStride; }
+
 constexpr int64_t kMostTokens = ((int64_t)1 << 31) - ((int64_t)1 << 16);
 
 /* What a shape is refused for; *nothing: there is no query and no key to work on. */
@@ -804,24 +990,39 @@ l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
     return launched();
 }
 
+/* Workgroups that share a tile of keys: as few (of the divisors of the heads that share it) as give every CU
+ * four.  Each more is a 32-bit copy of the gradients to write and to add up. */
+int splits_of(const Shape& s) {
+    const int64_t tiles = most_tiles(s.kv_tokens, s.images, kBackKeys) * s.kv_heads;
+    int splits = 1;
+    while (splits < s.group && (tiles * splits < 1024 || s.group % splits)) ++splits;
+    return splits;
+}
+
+size_t stats_bytes(const Shape& s) { return ((size_t)s.q_heads * (size_t)s.q_tokens * 2 * sizeof(float) + 15) / 16 * 16; }
+
 template <typename T>
 l3_status run_backward(const BackwardArgs& a, hipStream_t stream) {
     const int64_t q_grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
-    const int64_t kv_grid = most_tiles(a.s.kv_tokens, a.s.images, kBackKeys) * a.s.kv_heads;
-    const int64_t delta_grid = ((int64_t)a.s.q_tokens * a.s.q_heads * 16 + kThreads - 1) / kThreads;
-    if (q_grid >= (int64_t)1 << 31 || kv_grid >= (int64_t)1 << 31 || delta_grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
-    if (delta_grid) hipLaunchKernelGGL((l3_attention_delta_kernel<T>), dim3((unsigned)delta_grid), dim3(kThreads), 0, stream, a);
+    const int64_t kv_grid = most_tiles(a.s.kv_tokens, a.s.images, kBackKeys) * a.s.kv_heads * a.splits;
+    const int64_t stats_grid = ((int64_t)a.s.q_tokens * a.s.q_heads * 16 + kThreads - 1) / kThreads;
+    const int64_t join_grid = a.splits > 1 ? ((int64_t)a.s.kv_tokens * a.s.kv_heads * a.s.head_dim / 4 + kThreads - 1) / kThreads : 0;
+    if (q_grid >= (int64_t)1 << 31 || kv_grid >= (int64_t)1 << 31 || stats_grid >= (int64_t)1 << 31 || join_grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    if (stats_grid) hipLaunchKernelGGL((l3_attention_stats_kernel<T>), dim3((unsigned)stats_grid), dim3(kThreads), 0, stream, a);
     if (launched() != L3_OK) return L3_ERR_DEVICE;
     by_width(a.s.head_dim, [&](auto db) {
         by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
-            if (kv_grid)
-                hipLaunchKernelGGL((l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)kv_grid), dim3(kThreads), 0,
-                                   stream, a);
+            /* (queries first: they leave better deltas) */
             if (q_grid)
                 hipLaunchKernelGGL((l3_attention_q_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)q_grid), dim3(kThreads), 0,
                                    stream, a);
+            if (kv_grid)
+                hipLaunchKernelGGL((l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)kv_grid), dim3(kThreads), 0,
+                                   stream, a);
         });
     });
+    if (launched() != L3_OK) return L3_ERR_DEVICE;
+    if (join_grid) hipLaunchKernelGGL((l3_attention_kv_join_kernel<T>), dim3((unsigned)join_grid), dim3(kThreads), 0, stream, a);
     return launched();
 }
 
@@ -842,9 +1043,8 @@ l3_status run_step(const StepArgs& a, hipStream_t stream) {
         by_score(a.cap > 0.0f, a.slopes != nullptr, [&](auto cap, auto slopes) {
             const size_t tiles = kStepWaves * 4 * (size_t)kStepKeys * Tile<db.value>::kPitch;
             const size_t join = kStepWaves * (2 * 32 + 32 * db.value * 32) * sizeof(float);
-            const size_t lds = std::max(tiles, join);
-            const auto kernel = l3_attention_step_kernel<T, db.value, cap.value, slopes.value>;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kStepThreads), lds, stream, a);
+            hipLaunchKernelGGL((l3_attention_step_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kStepThreads),
+                               std::max(tiles, join), stream, a);
         });
     });
     if (launched() != L3_OK) return L3_ERR_DEVICE;
@@ -864,6 +1064,7 @@ l3_status l3_attention(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q,
     if (status != L3_OK) return status;
     if (nothing || shape->q_tokens == 0) return L3_OK;
     if (!good_heads(q) || !good_heads(out) || (shape->kv_tokens && (!good_heads(k) || !good_heads(v))) || !aligned(d_lse, 4)) return L3_ERR_INVALID_ARG;
+    if (far_apart(k) || far_apart(v)) return L3_ERR_LIMIT;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     const ForwardArgs a = {shape_of(*shape), heads_of(q), heads_of(k), heads_of(v), heads_of(out), d_lse};
@@ -873,7 +1074,9 @@ l3_status l3_attention(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q,
 size_t l3_attention_workspace(const l3_attention_shape* shape) {
     bool nothing = false;
     if (check_shape(shape, &nothing) != L3_OK) return 0;
-    return ((size_t)shape->q_heads * (size_t)shape->q_tokens * sizeof(float) + 15) / 16 * 16 + 16;
+    const Shape s = shape_of(*shape);
+    const size_t splits = (size_t)splits_of(s);
+    return 16 + stats_bytes(s) + (splits > 1 ? 2 * splits * (size_t)s.kv_tokens * s.kv_heads * s.head_dim * sizeof(float) : 0);
 }
 
 l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
@@ -889,10 +1092,12 @@ l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3
         return L3_ERR_INVALID_ARG;
     if (shape->kv_tokens && (!good_heads(k) || !good_heads(v) || !good_heads(k_grad) || !good_heads(v_grad))) return L3_ERR_INVALID_ARG;
     if (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < l3_attention_workspace(shape)) return L3_ERR_INVALID_ARG;
+    if (far_apart(q) || far_apart(out_grad) || far_apart(k) || far_apart(v)) return L3_ERR_LIMIT;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
-    const BackwardArgs a = {shape_of(*shape), heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(out_grad), heads_of(q_grad),
-                            heads_of(k_grad), heads_of(v_grad), d_lse, (float*)d_workspace};
+    const Shape s = shape_of(*shape);
+    const BackwardArgs a = {s, heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(out_grad), heads_of(q_grad),
+                            heads_of(k_grad), heads_of(v_grad), d_lse, (float*)d_workspace, (float*)((uint8_t*)d_workspace + stats_bytes(s)), splits_of(s)};
     return shape->dtype == L3_BF16 ? run_backward<__bf16>(a, (hipStream_t)stream) : run_backward<_Float16>(a, (hipStream_t)stream);
 }
 
@@ -917,6 +1122,7 @@ l3_status l3_attention_step(l3_ctx* ctx, int n, int head_dim, int q_heads, int k
         !aligned(d_lengths, 4) || !aligned(d_slopes, 4) || !d_workspace || !aligned(d_workspace, 16) ||
         workspace_bytes < l3_attention_step_workspace(n, head_dim, q_heads, kv_heads, max_length))
         return L3_ERR_INVALID_ARG;
+    if (far_apart(k_cache) || far_apart(v_cache)) return L3_ERR_LIMIT;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     StepArgs a = {heads_of(q), heads_of(k_cache), heads_of(v_cache), heads_of(out), k_sequence_stride, v_sequence_stride, d_lengths, d_slopes,
