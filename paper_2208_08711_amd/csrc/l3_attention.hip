@@ -512,6 +512,7 @@ __device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, co
     const ColumnPlace columns = reader.column + k_tile;
 #pragma unroll
     for (int b = 0; b < kKeys / 32; ++b) {
+        if (DB >= 3) __builtin_amdgcn_sched_barrier(0);    /* (one block after the other: registers are short) */
         f32x16 x = {}, dp = {};
 #pragma unroll
         for (int d = 0; d < 2 * DB; ++d) {
@@ -628,10 +629,22 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
 constexpr int kBackKeys = 128;             /* of a workgroup: 32 a wave */
 constexpr int kBackQueries = 32;           /* of a tile */
 
+/* Values as second operands: registers, or for wide heads, where these would leave room for one wave a
+ * SIMD only, rows of a tile in local memory. */
+template <typename T, int DB, bool IN_LDS>
+struct Values {
+    typename HalfVec<T, 8>::type held[IN_LDS ? 1 : 2 * DB];
+    uint32_t rows;
+    __device__ __forceinline__ typename HalfVec<T, 8>::type operator[](int d) const {
+        if constexpr (IN_LDS) return read_row<T, DB>(rows, 0, d);
+        else return held[d];
+    }
+};
+
 /* One tile of queries against the 32 keys of a wave.  stats: lse and delta of the tile's queries. */
-template <typename T, int DB, bool CAP, bool SLOPES, bool MASKED>
+template <typename T, int DB, bool CAP, bool SLOPES, bool MASKED, typename V>
 __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB], const typename HalfVec<T, 8>::type (&k)[2 * DB],
-                                             const typename HalfVec<T, 8>::type (&v)[2 * DB], const Reader<DB>& reader, uint32_t q_tile, uint32_t g_tile,
+                                             const V& v, const Reader<DB>& reader, uint32_t q_tile, uint32_t g_tile,
                                              const float* stats, const Shape& s, const Place& p, int prefix, int row0, int key, const Score& c, int lane) {
     const int half = lane >> 5;
     f32x16 x = {}, dp = {};
@@ -640,6 +653,7 @@ __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB],
         x = mfma(read_row<T, DB>(reader.row + q_tile, 0, d), k[d], x);
         dp = mfma(read_row<T, DB>(reader.row + g_tile, 0, d), v[d], dp);
     }
+    if (DB >= 3) __builtin_amdgcn_sched_barrier(0);    /* (nothing early: registers are short) */
     const float away = (float)(row0 + p.m - p.n - key + 4 * half);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -653,6 +667,7 @@ __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB],
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+        if (DB >= 3) __builtin_amdgcn_sched_barrier(0);
         const auto w = narrowed<T>(x, t), ds = narrowed<T>(dp, t);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
@@ -666,11 +681,13 @@ __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB],
  * them (or, split, of some of these).  S = Q K^T gives a lane 16 queries of its key, and P and dS are second
  * operands of dV^T = dO^T P and dK^T = Q^T dS as they are. */
 template <typename T, int DB, bool CAP, bool SLOPES>
-__global__ __launch_bounds__(kThreads, DB >= 3 ? 1 : 2) void l3_attention_kv_grad_kernel(BackwardArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(BackwardArgs a) {
     __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kBackQueries * Tile<DB>::kPitch];
     const uint32_t tiles_at = lds_address(tiles);
     const auto tile = [&](int buffer, int which) { return tiles_at + (2 * buffer + which) * (uint32_t)(kBackQueries * Tile<DB>::kPitch); };
     __shared__ __attribute__((aligned(16))) float stats[2][kBackQueries * 2];
+    constexpr bool kInLds = DB >= 3;
+    __shared__ __attribute__((aligned(256))) uint8_t value_tile[kInLds ? kBackKeys * Tile<DB>::kPitch : 16];
     const Shape& s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     int at = blockIdx.x;
@@ -684,13 +701,21 @@ __global__ __launch_bounds__(kThreads, DB >= 3 ? 1 : 2) void l3_attention_kv_gra
     const int key = tile0 + wave * 32 + (lane & 31);
     const int heads = s.group / a.splits, head0 = kv_head * s.group + split * heads;
 
-    typename HalfVec<T, 8>::type k[2 * DB], v[2 * DB];
+    const Reader<DB> reader(lane);
+    typename HalfVec<T, 8>::type k[2 * DB];
     load_operand<T, DB>(k, (const T*)a.k.d + (int64_t)(p.k0 + key) * a.k.token + (int64_t)kv_head * a.k.head, key < p.m, s.head_dim, half);
-    load_operand<T, DB>(v, (const T*)a.v.d + (int64_t)(p.k0 + key) * a.v.token + (int64_t)kv_head * a.v.head, key < p.m, s.head_dim, half);
+    Values<T, DB, kInLds> v;
+    if constexpr (kInLds) {
+        Fetch<DB, kBackKeys, kThreads> fetch_v;
+        fetch_v.set(a.v.token, s.head_dim, threadIdx.x);
+        fetch_v(lds_address(value_tile), (const T*)a.v.d + (int64_t)(p.k0 + tile0) * a.v.token + (int64_t)kv_head * a.v.head, p.m - tile0, threadIdx.x);
+        v.rows = lds_address(value_tile) + wave * 32 * Tile<DB>::kPitch + reader.row;
+    } else {
+        load_operand<T, DB>(v.held, (const T*)a.v.d + (int64_t)(p.k0 + key) * a.v.token + (int64_t)kv_head * a.v.head, key < p.m, s.head_dim, half);
+    }
     Fetch<DB, kBackQueries, kThreads> fetch_q, fetch_g;
     fetch_q.set(a.q.token, s.head_dim, threadIdx.x);
     fetch_g.set(a.out_grad.token, s.head_dim, threadIdx.x);
-    const Reader<DB> reader(lane);
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
