@@ -121,7 +121,7 @@ l3_status l3_rotation_turns(int pairs, double base, double factor, double origin
  * the way of the gradients).  k_heads = 0: queries only.  Outputs may be the inputs, element for element.
  * head_dim even, 2..L3_MAX_HEAD_DIM.  Any strides and alignment that an element needs; rows of 16-byte
  * aligned heads are fastest.
- * Errors: INVALID_ARG, LIMIT (2^31 tokens or more, more than 65535 heads), DEVICE. */
+ * Errors: INVALID_ARG, LIMIT (2^31 tokens or more, more than 1024 heads), DEVICE. */
 l3_status l3_rotate(l3_ctx* ctx, const l3_rotation* rotation, int inverse, int64_t tokens, int head_dim,
                     int q_heads, l3_heads q, l3_heads q_out, int k_heads, l3_heads k, l3_heads k_out,
                     l3_dtype dtype, void* stream);

@@ -26,7 +26,12 @@ bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) 
 
 /* A workgroup takes a strip: up to kStripPixels pixels' width of consecutive patches of one patch
  * row of one image, whose tokens lie end to end in the output.  The strip's pixel rows come into
- * local memory as they are; then every lane writes 16 bytes at a time, in the order of the output. */
+ * local memory as they are, four bytes a lane; then every lane gathers the bytes of 8 elements in the
+ * order of the output, looks their values up and writes 16 bytes.  RUN elements in a row (the most of 1, 2, 4, 8
+ * that divides the patch's side) belong to one row of a patch, so that places are worked out once for them. */
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
 constexpr int kTokenThreads = 256;
 constexpr uint32_t kStripPixels = 128;
 constexpr uint32_t kTokenImages = 64;      /* descriptors in the arguments of one launch */
@@ -49,6 +54,11 @@ struct TokenArgs {
     uint32_t side, per_strip;              /* patches of a full strip */
 };
 
+/* e / d for e * d below 2^32, by r = ceil(2^32 / d) (0 stands for d = 1). */
+__device__ __forceinline__ uint32_t reciprocal(uint32_t d) { return 0xFFFFFFFFu / d + 1; }
+__device__ __forceinline__ uint32_t quotient(uint32_t e, uint32_t d, uint32_t r) { return d == 1 ? e : __umulhi(e, r); }
+
+template <uint32_t RUN>
 __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArgs a) {
     extern __shared__ uint8_t lds[];
     uint16_t* const table = reinterpret_cast<uint16_t*>(lds);
@@ -73,11 +83,20 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     for (uint32_t i = tid; i < 768; i += kTokenThreads) table[i] = a.table[i];
     const uint32_t x0 = col0 * side, y0 = row * side;
     const uint32_t width = min(count * side, im.width - x0), height = min(side, im.height - y0);   /* inside the image */
-    const uint32_t pitch = a.per_strip * side * 3;
-    const uint32_t bytes = width * 3;
-    for (uint32_t y = tid / 64; y < height; y += kTokenThreads / 64) {
-        const uint8_t* src = im.rgb + (uint64_t)(y0 + y) * im.row_stride + (uint64_t)x0 * 3;
-        for (uint32_t b = tid % 64; b < bytes; b += 64) strip[y * pitch + b] = src[b];
+    const uint32_t pitch = (a.per_strip * side * 3 + 3) & ~3u;
+    const uint32_t bytes = width * 3, words = (bytes + 3) / 4, by_words = reciprocal(words);
+    const uint8_t* const corner = im.rgb + (uint64_t)y0 * im.row_stride + (uint64_t)x0 * 3;
+#pragma unroll 4
+    for (uint32_t i = tid; i < words * height; i += kTokenThreads) {
+        const uint32_t y = quotient(i, words, by_words), b = (i - y * words) * 4;
+        const uint8_t* src = corner + (uint64_t)y * im.row_stride + b;
+        uint32_t v = 0;
+        if (b + 4 <= bytes) {
+            v = *reinterpret_cast<const u32_any*>(src);
+        } else {
+            for (uint32_t k = 0; b + k < bytes; ++k) v |= (uint32_t)src[k] << (8 * k);
+        }
+        *reinterpret_cast<uint32_t*>(strip + y * pitch + b) = v;
     }
     if (a.positions)
         for (uint32_t t = tid; t < count; t += kTokenThreads) {
@@ -92,12 +111,36 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     __syncthreads();
 
     const uint32_t area = side * side, size = 3 * area, total = count * size;
-    uint16_t* const out = a.tokens + (uint64_t)token0 * size;
-    for (uint32_t e0 = tid; e0 < total; e0 += kTokenThreads) {
-        const uint32_t t = e0 / size, r = e0 - t * size;
-        const uint32_t c = r / area, r2 = r - c * area;
-        const uint32_t y = r2 / side, x = t * side + (r2 - y * side);
-        out[e0] = (x < width && y < height) ? table[c * 256 + strip[y * pitch + 3 * x + c]] : (uint16_t)0;
+    const uint32_t by_size = reciprocal(size), by_area = reciprocal(area), by_side = reciprocal(side);
+    const uint64_t e0 = (uint64_t)token0 * size;
+    const uint32_t lead = (uint32_t)(e0 & 7u);          /* of the first 16 bytes, elements of the strip before */
+    uint16_t* const out = a.tokens + (e0 - lead);
+    const bool ragged = width < count * side || height < side;
+    for (uint32_t g = tid * 8; g < lead + total; g += kTokenThreads * 8) {
+        uint32_t packed[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i += RUN) {
+            /* (places outside the strip read some byte of it) */
+            const uint32_t e = min(g + i - min(lead, g + i), total - RUN);
+            const uint32_t t = quotient(e, size, by_size), r = e - t * size;
+            const uint32_t c = quotient(r, area, by_area), r2 = r - c * area;
+            const uint32_t y = quotient(r2, side, by_side), x = t * side + (r2 - y * side);
+            const uint32_t at = (y < height ? y * pitch : 0u) + 3 * x + c, values = c * 256;
+#pragma unroll
+            for (uint32_t k = 0; k < RUN; ++k) {
+                uint32_t v = table[values + strip[at + 3 * k]];
+                if (ragged && (x + k >= width || y >= height)) v = 0;
+                if ((i + k) & 1) packed[(i + k) / 2] |= v << 16;
+                else packed[(i + k) / 2] = v;
+            }
+        }
+        if (g >= lead && g + 8 <= lead + total) {
+            *reinterpret_cast<u32x4*>(out + g) = u32x4{packed[0], packed[1], packed[2], packed[3]};
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                if (g + i >= lead && g + i < lead + total) out[g + i] = (uint16_t)(packed[i / 2] >> (16 * (i & 1)));
+        }
     }
 }
 
@@ -199,8 +242,10 @@ l3_status launch_dropout(const DropoutArgs& a, bool wide, hipStream_t stream) {
 
 /* A head's elements as pairs: pair j < pairs is (j, j + pairs) or, interleaved, (2j, 2j + 1) and is
  * turned; the others, (2j, 2j + 1), pass through.  A lane takes V consecutive pairs, which are two
- * runs of V elements; `lanes` lanes (a power of two) take a head, and a slot of them the same pairs of
- * several heads of one token, so that sines and cosines are worked out once for these. */
+ * runs of V elements; `lanes` lanes (a power of two) take a head, and a slot of them the same pairs of up to
+ * `per_slot` heads of one token and tensor, so that sines and cosines are worked out once for these, with all
+ * their loads on the way together.  A slot keeps its heads from token to token (the launch's slots are
+ * a multiple of a token's), so weights are read, and their gradients kept, once. */
 struct RotateTensor {
     const void* x;
     void* y;
@@ -217,11 +262,13 @@ struct RotateArgs {
     float* partial;                        /* backward: [blocks][2][head_dim] */
     int32_t head_dim, pairs, axes, interleaved, inverse;
     int32_t lanes, chunks;                 /* lanes of a head; those of them that have pairs */
-    int32_t per_slot, slots_per_token;     /* heads of a slot */
+    int32_t q_slots, slots;                /* of a token: those of the queries, all */
     float magnitude, eps;
     uint64_t turns[L3_MAX_HEAD_DIM / 2];
 };
 
+constexpr int kMostHeads = 1024;
+constexpr int64_t kManyThreads = 1 << 18;
 enum { kRotate = 0, kNormRotate = 1, kNormRotateBack = 2 };
 constexpr int kRotateThreads = 256;
 constexpr int kBackBlocks = 1024;          /* most blocks of the backward kernel, which sets the workspace */
@@ -234,9 +281,14 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 }
 
 template <typename T, int V>
-__device__ __forceinline__ void load_pairs(const T* head, int a, int b, float (&x)[2][V]) {
-    load_wide<T, V>(head + a, x[0]);
-    load_wide<T, V>(head + b, x[1]);
+__device__ __forceinline__ void widen(const typename HalfVec<T, V>::type (&h)[2], float (&x)[2][V], bool there) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (V == 1) x[k][i] = there ? (float)h[k] : 0.0f;
+            else x[k][i] = there ? (float)h[k][i] : 0.0f;
+        }
 }
 
 /* The two runs as (first, second) elements of the pairs: as they are in the half layout, every other
@@ -273,12 +325,16 @@ __device__ __forceinline__ void from_pairs(float (&x)[2][V], bool side_by_side) 
     }
 }
 
-template <typename T, int V, int MODE>
+template <typename T, int V, int MODE, int PER_SLOT>
 __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a) {
     const int lane = threadIdx.x & (a.lanes - 1);
     const bool active = lane < a.chunks;
-    const int64_t slots = a.tokens * a.slots_per_token;
-    const int64_t step = (int64_t)gridDim.x * (kRotateThreads / a.lanes);
+    const int64_t here = (int64_t)blockIdx.x * (kRotateThreads / a.lanes) + threadIdx.x / a.lanes;
+    const int slot = (int)(here % a.slots);
+    const int64_t step = (int64_t)gridDim.x * (kRotateThreads / a.lanes) / a.slots;
+    const int which = slot >= a.q_slots;
+    const RotateTensor t = a.t[which];
+    const int h0 = (slot - (which ? a.q_slots : 0)) * PER_SLOT;
     const int j0 = active ? lane * V : 0;                      /* first pair */
     const bool turned = j0 < a.pairs;
     const bool side_by_side = !turned || a.interleaved;
@@ -288,13 +344,32 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
 #pragma unroll
     for (int i = 0; i < V; ++i) turns[i] = turned ? a.turns[j0 + i] : 0u;
     const int axis = a.axes == 2 && j0 >= a.pairs / 2 ? 1 : 0;    /* V divides pairs/axes */
-    const int heads = a.t[0].heads + a.t[1].heads;
-    float sum[2][2][V] = {};                                   /* backward: gradients of both weights */
+    const float magnitude = turned ? a.magnitude : 1.0f, by_dim = 1.0f / (float)a.head_dim;
+    float w[2][V], sum[2][V] = {};                             /* weights; backward: their gradients */
+    if (MODE != kRotate) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const bool there = active && h0 < t.heads;
+            w[0][i] = there ? t.weight[side_by_side ? 2 * (j0 + i) : j0 + i] : 0.0f;
+            w[1][i] = there ? t.weight[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] : 0.0f;
+        }
+    }
 
-    for (int64_t slot = (int64_t)blockIdx.x * (kRotateThreads / a.lanes) + threadIdx.x / a.lanes; slot < slots; slot += step) {
-        const int64_t token = a.slots_per_token == 1 ? slot : slot / a.slots_per_token;
-        const int h0 = (int)(slot - token * a.slots_per_token) * a.per_slot;
-        const int h1 = min(h0 + a.per_slot, heads);
+    for (int64_t token = here / a.slots; token < a.tokens; token += step) {
+        const T* const from = (const T*)t.x + token * t.x_token + h0 * t.x_head;
+        const T* const grads = (const T*)t.grad + token * t.grad_token + h0 * t.grad_head;
+        T* const to = (T*)t.y + token * t.y_token + h0 * t.y_head;
+        typename HalfVec<T, V>::type xs[PER_SLOT][2], gs[PER_SLOT][2];
+#pragma unroll
+        for (int h = 0; h < PER_SLOT; ++h) {
+            if (!active || h0 + h >= t.heads) continue;
+            xs[h][0] = *(const typename HalfVec<T, V>::type*)(from + h * t.x_head + ea);
+            xs[h][1] = *(const typename HalfVec<T, V>::type*)(from + h * t.x_head + eb);
+            if (MODE == kNormRotateBack) {
+                gs[h][0] = *(const typename HalfVec<T, V>::type*)(grads + h * t.grad_head + ea);
+                gs[h][1] = *(const typename HalfVec<T, V>::type*)(grads + h * t.grad_head + eb);
+            }
+        }
         float cs[V], sn[V];
         const int64_t position = turned ? (int64_t)a.positions[token * a.axes + axis] : 0;
 #pragma unroll
@@ -303,31 +378,23 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
              * the sine and cosine instructions take */
             const uint64_t angle = (uint64_t)position * turns[i];
             const float f = (float)(int32_t)(angle >> 32) * 0x1p-32f;
-            const float m = turned ? a.magnitude : 1.0f;
-            cs[i] = __builtin_amdgcn_cosf(f) * m;
-            sn[i] = __builtin_amdgcn_sinf(f) * m;
+            cs[i] = __builtin_amdgcn_cosf(f) * magnitude;
+            sn[i] = __builtin_amdgcn_sinf(f) * magnitude;
             if (a.inverse) sn[i] = -sn[i];
         }
-        for (int h = h0; h < h1; ++h) {
-            const int which = h >= a.t[0].heads;
-            const RotateTensor& t = a.t[which];
-            const int64_t head = h - (which ? a.t[0].heads : 0);
-            float x[2][V], r[2][V];
-            if (active) load_pairs<T, V>((const T*)t.x + token * t.x_token + head * t.x_head, ea, eb, x);
-            else for (int i = 0; i < V; ++i) x[0][i] = x[1][i] = 0.0f;
-            to_pairs<V>(x, side_by_side);
-            float w[2][V];
-            if (MODE != kRotate) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    w[0][i] = active ? t.weight[side_by_side ? 2 * (j0 + i) : j0 + i] : 0.0f;
-                    w[1][i] = active ? t.weight[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] : 0.0f;
-                }
+        for (int h = 0; h < PER_SLOT; ++h) {
+            /* (the lanes of a head are of one mind about this, and those of other heads do not matter
+             * to the sums below) */
+            if (h0 + h >= t.heads) continue;
+            float x[2][V], r[2][V];
+            widen<T, V>(xs[h], x, active);
+            to_pairs<V>(x, side_by_side);
+            if (MODE != kRotate) {
                 float squares = 0.0f;
 #pragma unroll
-                for (int i = 0; i < V; ++i) squares += x[0][i] * x[0][i] + x[1][i] * x[1][i];
-                const float mean = head_sum(squares, a.lanes) / (float)a.head_dim;
-                const float rstd = 1.0f / sqrtf(mean + a.eps);
+                for (int i = 0; i < V; ++i) squares = __builtin_fmaf(x[0][i], x[0][i], __builtin_fmaf(x[1][i], x[1][i], squares));
+                const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(head_sum(squares, a.lanes), by_dim, a.eps));
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     x[0][i] *= rstd;
@@ -335,27 +402,24 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
                 }
                 if (MODE == kNormRotateBack) {
                     float g[2][V];
-                    if (active) load_pairs<T, V>((const T*)t.grad + token * t.grad_token + head * t.grad_head, ea, eb, g);
-                    else for (int i = 0; i < V; ++i) g[0][i] = g[1][i] = 0.0f;
+                    widen<T, V>(gs[h], g, active);
                     to_pairs<V>(g, side_by_side);
                     float dot = 0.0f;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float ga = turned ? g[0][i] * cs[i] - g[1][i] * sn[i] : g[0][i];
-                        const float gb = turned ? g[0][i] * sn[i] + g[1][i] * cs[i] : g[1][i];
-                        sum[0][0][i] += which ? 0.0f : ga * x[0][i];
-                        sum[0][1][i] += which ? 0.0f : gb * x[1][i];
-                        sum[1][0][i] += which ? ga * x[0][i] : 0.0f;
-                        sum[1][1][i] += which ? gb * x[1][i] : 0.0f;
+                        const float ga = turned ? __builtin_fmaf(g[0][i], cs[i], -g[1][i] * sn[i]) : g[0][i];
+                        const float gb = turned ? __builtin_fmaf(g[0][i], sn[i], g[1][i] * cs[i]) : g[1][i];
+                        sum[0][i] = __builtin_fmaf(ga, x[0][i], sum[0][i]);
+                        sum[1][i] = __builtin_fmaf(gb, x[1][i], sum[1][i]);
                         g[0][i] = ga * w[0][i];
                         g[1][i] = gb * w[1][i];
-                        dot += g[0][i] * x[0][i] + g[1][i] * x[1][i];
+                        dot = __builtin_fmaf(g[0][i], x[0][i], __builtin_fmaf(g[1][i], x[1][i], dot));
                     }
-                    dot = head_sum(dot, a.lanes) / (float)a.head_dim;
+                    dot = head_sum(dot, a.lanes) * by_dim;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        r[0][i] = rstd * (g[0][i] - x[0][i] * dot);
-                        r[1][i] = rstd * (g[1][i] - x[1][i] * dot);
+                        r[0][i] = rstd * __builtin_fmaf(-x[0][i], dot, g[0][i]);
+                        r[1][i] = rstd * __builtin_fmaf(-x[1][i], dot, g[1][i]);
                     }
                 } else {
 #pragma unroll
@@ -368,40 +432,47 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
             if (MODE != kNormRotateBack) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    r[0][i] = turned ? x[0][i] * cs[i] - x[1][i] * sn[i] : x[0][i];
-                    r[1][i] = turned ? x[0][i] * sn[i] + x[1][i] * cs[i] : x[1][i];
+                    r[0][i] = turned ? __builtin_fmaf(x[0][i], cs[i], -x[1][i] * sn[i]) : x[0][i];
+                    r[1][i] = turned ? __builtin_fmaf(x[0][i], sn[i], x[1][i] * cs[i]) : x[1][i];
                 }
             }
             from_pairs<V>(r, side_by_side);
             if (active) {
-                T* const out = (T*)t.y + token * t.y_token + head * t.y_head;
-                store_narrow<T, V>(out + ea, r[0]);
-                store_narrow<T, V>(out + eb, r[1]);
+                store_narrow<T, V>(to + h * t.y_head + ea, r[0]);
+                store_narrow<T, V>(to + h * t.y_head + eb, r[1]);
             }
         }
     }
 
     if (MODE == kNormRotateBack) {
-        /* every thread's sums into local memory, one column per element, then columns top to bottom */
+        /* every thread's sums into local memory, then those of one element top to bottom, the queries'
+         * and the keys' apart */
         __shared__ float room[kRotateThreads * 2];
+        __shared__ uint8_t of_keys[kRotateThreads];
         const int groups = kRotateThreads / a.lanes;
-        for (int which = 0; which < 2; ++which)
-            for (int i = 0; i < V; ++i) {
-                __syncthreads();
-                room[threadIdx.x * 2] = sum[which][0][i];
-                room[threadIdx.x * 2 + 1] = sum[which][1][i];
-                __syncthreads();
-                if ((int)threadIdx.x < a.lanes && active) {
-                    float s0 = 0.0f, s1 = 0.0f;
-                    for (int g = 0; g < groups; ++g) {
-                        s0 += room[(g * a.lanes + lane) * 2];
-                        s1 += room[(g * a.lanes + lane) * 2 + 1];
-                    }
-                    float* const out = a.partial + ((int64_t)blockIdx.x * 2 + which) * a.head_dim;
-                    out[side_by_side ? 2 * (j0 + i) : j0 + i] = s0;
-                    out[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] = s1;
+        if (lane == 0) of_keys[threadIdx.x / a.lanes] = (uint8_t)which;
+        for (int i = 0; i < V; ++i) {
+            __syncthreads();
+            room[threadIdx.x * 2] = sum[0][i];
+            room[threadIdx.x * 2 + 1] = sum[1][i];
+            __syncthreads();
+            if ((int)threadIdx.x < a.lanes && active) {
+                float s[2][2] = {};
+                for (int g = 0; g < groups; ++g) {
+                    const float s0 = room[(g * a.lanes + lane) * 2], s1 = room[(g * a.lanes + lane) * 2 + 1];
+                    const bool k = of_keys[g];
+                    s[0][0] += k ? 0.0f : s0;
+                    s[0][1] += k ? 0.0f : s1;
+                    s[1][0] += k ? s0 : 0.0f;
+                    s[1][1] += k ? s1 : 0.0f;
+                }
+                for (int k = 0; k < 2; ++k) {
+                    float* const out = a.partial + ((int64_t)blockIdx.x * 2 + k) * a.head_dim;
+                    out[side_by_side ? 2 * (j0 + i) : j0 + i] = s[k][0];
+                    out[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] = s[k][1];
                 }
             }
+        }
     }
 }
 
@@ -423,12 +494,21 @@ __global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const fl
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, int PER_SLOT>
 void launch_rotate(const RotateArgs& a, int mode, unsigned grid, hipStream_t stream) {
     const dim3 threads(kRotateThreads);
-    if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate>), dim3(grid), threads, 0, stream, a);
-    else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate>), dim3(grid), threads, 0, stream, a);
-    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack>), dim3(grid), threads, 0, stream, a);
+    if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
+    else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
+    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, PER_SLOT>), dim3(grid), threads, 0, stream, a);
+}
+
+template <typename T>
+void launch_rotate(const RotateArgs& a, int v, int per_slot, int mode, unsigned grid, hipStream_t stream) {
+    if (v == 8 && per_slot == 4) launch_rotate<T, 8, 4>(a, mode, grid, stream);
+    else if (v == 8) launch_rotate<T, 8, 1>(a, mode, grid, stream);
+    else if (v == 4 && per_slot == 4) launch_rotate<T, 4, 4>(a, mode, grid, stream);
+    else if (v == 4) launch_rotate<T, 4, 1>(a, mode, grid, stream);
+    else launch_rotate<T, 1, 1>(a, mode, grid, stream);
 }
 
 bool good_heads(const l3_heads& h) { return h.d && aligned(h.d, 2) && h.token_stride >= 0 && h.head_stride >= 0; }
@@ -461,7 +541,7 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
         if (mode != kRotate && !side[s].weight) return L3_ERR_INVALID_ARG;
         if (mode == kNormRotateBack && !good_heads(side[s].grad)) return L3_ERR_INVALID_ARG;
     }
-    if (tokens >= (int64_t)1 << 31 || side[0].heads > 65535 || side[1].heads > 65535) return L3_ERR_LIMIT;
+    if (tokens >= (int64_t)1 << 31 || side[0].heads > kMostHeads || side[1].heads > kMostHeads) return L3_ERR_LIMIT;
     if (!work && mode != kNormRotateBack) return L3_OK;
 
     RotateArgs a = {};
@@ -503,25 +583,25 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     a.magnitude = rot->magnitude;
     a.eps = eps;
     if (rot->pairs) std::memcpy(a.turns, rot->turns, (size_t)rot->pairs * 8);
-    const int heads = side[0].heads + side[1].heads;
-    a.per_slot = 1;
-    a.slots_per_token = heads > 0 ? heads : 1;
-    const int64_t slots = a.tokens * a.slots_per_token;
-    int64_t grid = (slots * a.lanes + kRotateThreads - 1) / kRotateThreads;
-    grid = std::max<int64_t>(1, std::min<int64_t>(grid, mode == kNormRotateBack ? kBackBlocks : 16384));
+    /* Four heads a slot, where one of them each would still give all CUs their threads */
+    const int64_t heads = side[0].heads + side[1].heads;
+    const int per_slot = v > 1 && a.tokens * heads * a.lanes >= kManyThreads ? 4 : 1;
+    a.q_slots = (side[0].heads + per_slot - 1) / per_slot;
+    a.slots = std::max(1, a.q_slots + (side[1].heads + per_slot - 1) / per_slot);
+    /* whole tokens: the launch's slots are a multiple of a token's */
+    const int in_block = kRotateThreads / a.lanes;
+    if (a.slots > kBackBlocks / 2) a.slots = (a.slots + 3) / 4 * 4;        /* (idle slots, to be no more workgroups than this) */
+    int unit = a.slots;
+    for (int g = in_block; g > 1 && unit % 2 == 0; g /= 2) unit /= 2;      /* (in_block is a power of two, 4 or more) */
+    const int64_t wanted = (a.tokens * a.slots + in_block - 1) / in_block, most = mode == kNormRotateBack ? kBackBlocks : 16384;
+    int64_t grid = std::min(wanted, most) / unit * unit;
+    if (grid < std::min(wanted, most) && (grid + unit <= most || grid == 0)) grid += unit;
 
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     const hipStream_t st = (hipStream_t)stream;
-    if (dtype == L3_BF16) {
-        if (v == 8) launch_rotate<__bf16, 8>(a, mode, (unsigned)grid, st);
-        else if (v == 4) launch_rotate<__bf16, 4>(a, mode, (unsigned)grid, st);
-        else launch_rotate<__bf16, 1>(a, mode, (unsigned)grid, st);
-    } else {
-        if (v == 8) launch_rotate<_Float16, 8>(a, mode, (unsigned)grid, st);
-        else if (v == 4) launch_rotate<_Float16, 4>(a, mode, (unsigned)grid, st);
-        else launch_rotate<_Float16, 1>(a, mode, (unsigned)grid, st);
-    }
+    if (grid && dtype == L3_BF16) launch_rotate<__bf16>(a, v, per_slot, mode, (unsigned)grid, st);
+    else if (grid) launch_rotate<_Float16>(a, v, per_slot, mode, (unsigned)grid, st);
     if (mode == kNormRotateBack) {
         if (launched() != L3_OK) return L3_ERR_DEVICE;
         hipLaunchKernelGGL(l3_weight_grad_kernel, dim3((unsigned)(2 * head_dim)), dim3(kRotateThreads), 0, st, partial, (int)grid,
@@ -572,7 +652,9 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
     a.end_token = (uint32_t)total;
     a.side = side;
     a.per_strip = std::max(1u, kStripPixels / side);
-    const size_t lds = 768 * 2 + (size_t)a.per_strip * side * 3 * side;
+    /* (behind the last row: what the gather reads for places outside the image) */
+    const size_t lds = 768 * 2 + (size_t)((a.per_strip * side * 3 + 3) / 4 * 4) * side + 32;
+    const auto kernel = side % 8 == 0 ? l3_patch_tokens_kernel<8> : side % 4 == 0 ? l3_patch_tokens_kernel<4> : side % 2 == 0 ? l3_patch_tokens_kernel<2> : l3_patch_tokens_kernel<1>;
     uint32_t first = 0;
     for (int i0 = 0; i0 < n; i0 += (int)kTokenImages) {
         a.images = (uint32_t)std::min<int>((int)kTokenImages, n - i0);
@@ -586,7 +668,7 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
             first += cols * rows;
         }
         for (uint32_t i = a.images; i < kTokenImages; ++i) a.image[i] = {};
-        hipLaunchKernelGGL(l3_patch_tokens_kernel, dim3(blocks), dim3(kTokenThreads), lds, (hipStream_t)stream, a);
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kTokenThreads), lds, (hipStream_t)stream, a);
         if (launched() != L3_OK) return L3_ERR_DEVICE;
     }
     return L3_OK;

@@ -280,6 +280,31 @@ def test_norm_rotate_many_tokens(l3, ctx, tokens, heads):
     assert bool(((wg.cpu().double() - gw).abs() <= ref.SLACK * gw_size).all())
 
 
+@pytest.mark.parametrize("heads", ((1001, 1), (13, 1024), (0, 7)))
+def test_norm_rotate_many_heads(l3, ctx, heads):
+    """More heads than one workgroup, or all of them, have slots for; and no queries at all."""
+    hq, hk = heads
+    tokens, d = 150, 8
+    x, g = [normal((tokens, h, d), 80 + h, torch.bfloat16) for h in heads], [normal((tokens, h, d), 81 + h, torch.bfloat16) for h in heads]
+    w = [1 + 0.2 * normal((d,), 82 + i, torch.float32) for i in range(2)]
+    rotation, where = l3.Rotation(l3.rotation_turns(4)), torch.arange(tokens, dtype=torch.int32)
+    out, back, wg = [torch.empty_like(t) for t in x], [torch.empty_like(t) for t in x], [torch.full_like(t, 5.0) for t in w]
+    l3.norm_rotate(ctx, rotation, where.cuda(), x[0], w[0], out[0], x[1], w[1], out[1])
+    l3.norm_rotate_backward(ctx, rotation, where.cuda(), x[0], w[0], g[0], back[0], wg[0], x[1], w[1], g[1], back[1], wg[1])
+    angle = ref.angles(l3.rotation_turns(4), 1, where)
+    for i in range(2):
+        if not heads[i]:
+            continue
+        xd, wd, gd = x[i].cpu().double(), w[i].cpu().double(), g[i].cpu().double()
+        want, size = ref.turned(ref.normed(xd, wd, 1e-6), angle, 4, False, 1.0)
+        ref.close(out[i], want, ref.SLACK * size, "norm_rotate")
+        turned, most = ref.turned(gd, angle, 4, False, 1.0, back=True)
+        gx, gx_size, gw, _ = ref.norm_back(xd, wd, 1e-6, turned)
+        _, big, _, gw_size = ref.norm_back(xd, wd, 1e-6, most)
+        ref.close(back[i], gx, ref.SLACK * torch.maximum(gx_size, big), "gradient of x")
+        assert bool(((wg[i].cpu().double() - gw).abs() <= ref.SLACK * gw_size).all())
+
+
 # ---- attention ----------------------------------------------------------------------------------
 
 
