@@ -25,12 +25,15 @@ bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) 
  * ------------------------------------------------------------------------ */
 
 /* A workgroup takes a strip: up to kStripPixels pixels' width of consecutive patches of one patch
- * row of one image, whose tokens lie end to end in the output.  The strip's pixel rows come into
- * local memory as they are, four bytes a lane; then every lane gathers the bytes of 8 elements in the
- * order of the output, looks their values up and writes 16 bytes.  RUN elements in a row (the most of 1, 2, 4, 8
- * that divides the patch's side) belong to one row of a patch, so that places are worked out once for them. */
+ * row of one image, whose tokens lie end to end in the output.  A lane takes four pixels (12 bytes) of a row,
+ * looks the values of their bytes up and puts them, channel by channel, where they belong in an image of the
+ * output in local memory, RUN pixels of a patch's row at a time; from there whole lines go out, PIECE
+ * elements at a time (a patch is a multiple of that).  RUN, PIECE: 4, 8 where 4 divides the side, 2, 4
+ * for other even sides, else 1, 1. */
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
+typedef u32x3 u32x3_any __attribute__((aligned(1)));
 
 constexpr int kTokenThreads = 256;
 constexpr uint32_t kStripPixels = 128;
@@ -54,15 +57,19 @@ struct TokenArgs {
     uint32_t side, per_strip;              /* patches of a full strip */
 };
 
+/* Bytes from patch to patch in local memory: a multiple of 16, and such that one row of the patches of
+ * a strip is spread over the banks. */
+__host__ __device__ constexpr uint32_t patch_pitch(uint32_t size) { return (size * 2 + 15) / 16 * 16 + 32; }
+
 /* e / d for e * d below 2^32, by r = ceil(2^32 / d) (0 stands for d = 1). */
 __device__ __forceinline__ uint32_t reciprocal(uint32_t d) { return 0xFFFFFFFFu / d + 1; }
 __device__ __forceinline__ uint32_t quotient(uint32_t e, uint32_t d, uint32_t r) { return d == 1 ? e : __umulhi(e, r); }
 
-template <uint32_t RUN>
+template <uint32_t RUN, uint32_t PIECE>
 __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArgs a) {
-    extern __shared__ uint8_t lds[];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     uint16_t* const table = reinterpret_cast<uint16_t*>(lds);
-    uint8_t* const strip = lds + 768 * 2;
+    uint8_t* const patches = lds + 768 * 2;
     const uint32_t tid = threadIdx.x;
 
     /* which image: the first whose blocks end behind this one */
@@ -83,21 +90,9 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     for (uint32_t i = tid; i < 768; i += kTokenThreads) table[i] = a.table[i];
     const uint32_t x0 = col0 * side, y0 = row * side;
     const uint32_t width = min(count * side, im.width - x0), height = min(side, im.height - y0);   /* inside the image */
-    const uint32_t pitch = (a.per_strip * side * 3 + 3) & ~3u;
-    const uint32_t bytes = width * 3, words = (bytes + 3) / 4, by_words = reciprocal(words);
+    const uint32_t area = side * side, size = 3 * area, pitch = patch_pitch(size);
+    const uint32_t quads = (count * side + 3) / 4, by_quads = reciprocal(quads), by_side = reciprocal(side);
     const uint8_t* const corner = im.rgb + (uint64_t)y0 * im.row_stride + (uint64_t)x0 * 3;
-#pragma unroll 4
-    for (uint32_t i = tid; i < words * height; i += kTokenThreads) {
-        const uint32_t y = quotient(i, words, by_words), b = (i - y * words) * 4;
-        const uint8_t* src = corner + (uint64_t)y * im.row_stride + b;
-        uint32_t v = 0;
-        if (b + 4 <= bytes) {
-            v = *reinterpret_cast<const u32_any*>(src);
-        } else {
-            for (uint32_t k = 0; b + k < bytes; ++k) v |= (uint32_t)src[k] << (8 * k);
-        }
-        *reinterpret_cast<uint32_t*>(strip + y * pitch + b) = v;
-    }
     if (a.positions)
         for (uint32_t t = tid; t < count; t += kTokenThreads) {
             int32_t* p = a.positions + 2 * (uint64_t)(token0 + t);
@@ -110,28 +105,63 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     }
     __syncthreads();
 
-    const uint32_t area = side * side, size = 3 * area, total = count * size;
-    const uint32_t by_size = reciprocal(size), by_area = reciprocal(area), by_side = reciprocal(side);
+#pragma unroll 2
+    for (uint32_t i = tid; i < quads * side; i += kTokenThreads) {
+        const uint32_t y = quotient(i, quads, by_quads), x = (i - y * quads) * 4;
+        uint32_t v[3] = {};
+        const uint32_t inside = y < height && x < width ? min(4u, width - x) : 0u;    /* pixels */
+        const uint8_t* const src = corner + (uint64_t)y * im.row_stride + 3 * x;
+        if (inside == 4) {
+            const u32x3_any w = *reinterpret_cast<const u32x3_any*>(src);
+#pragma unroll
+            for (uint32_t k = 0; k < 3; ++k) v[k] = w[k];
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < 9; ++k)
+                if (k < 3 * inside) v[k / 4] |= (uint32_t)src[k] << (8 * (k % 4));
+        }
+        uint32_t value[3][4];
+#pragma unroll
+        for (uint32_t k = 0; k < 12; ++k) {
+            const uint32_t found = table[(k % 3) * 256 + ((v[k / 4] >> (8 * (k % 4))) & 255u)];
+            value[k % 3][k / 3] = k / 3 < inside ? found : 0u;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k += RUN) {
+            const uint32_t t = quotient(x + k, side, by_side);
+            if (RUN < 4 && t >= count) break;
+            uint8_t* const to = patches + t * pitch + 2 * (y * side + (x + k - t * side));
+#pragma unroll
+            for (uint32_t c = 0; c < 3; ++c) {
+                if (RUN == 4) *reinterpret_cast<u32x2*>(to + 2 * c * area) = u32x2{value[c][0] | value[c][1] << 16, value[c][2] | value[c][3] << 16};
+                else if (RUN == 2) *reinterpret_cast<uint32_t*>(to + 2 * c * area) = value[c][k] | value[c][k + 1] << 16;
+                else *reinterpret_cast<uint16_t*>(to + 2 * c * area) = (uint16_t)value[c][k];
+            }
+        }
+    }
+    __syncthreads();
+
+    const uint32_t total = count * size, by_size = reciprocal(size);
     const uint64_t e0 = (uint64_t)token0 * size;
     const uint32_t lead = (uint32_t)(e0 & 7u);          /* of the first 16 bytes, elements of the strip before */
     uint16_t* const out = a.tokens + (e0 - lead);
-    const bool ragged = width < count * side || height < side;
     for (uint32_t g = tid * 8; g < lead + total; g += kTokenThreads * 8) {
-        uint32_t packed[4];
+        uint32_t packed[4] = {};
 #pragma unroll
-        for (uint32_t i = 0; i < 8; i += RUN) {
-            /* (places outside the strip read some byte of it) */
-            const uint32_t e = min(g + i - min(lead, g + i), total - RUN);
-            const uint32_t t = quotient(e, size, by_size), r = e - t * size;
-            const uint32_t c = quotient(r, area, by_area), r2 = r - c * area;
-            const uint32_t y = quotient(r2, side, by_side), x = t * side + (r2 - y * side);
-            const uint32_t at = (y < height ? y * pitch : 0u) + 3 * x + c, values = c * 256;
+        for (uint32_t i = 0; i < 8; i += PIECE) {
+            if (g + i < lead || g + i >= lead + total) continue;
+            const uint32_t e = g + i - lead, t = quotient(e, size, by_size);
+            const uint8_t* const from = patches + t * pitch + 2 * (e - t * size);
+            if (PIECE == 8) {
+                const u32x4 p = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
-            for (uint32_t k = 0; k < RUN; ++k) {
-                uint32_t v = table[values + strip[at + 3 * k]];
-                if (ragged && (x + k >= width || y >= height)) v = 0;
-                if ((i + k) & 1) packed[(i + k) / 2] |= v << 16;
-                else packed[(i + k) / 2] = v;
+                for (uint32_t k = 0; k < 4; ++k) packed[k] = p[k];
+            } else if (PIECE == 4) {
+                const u32x2 p = *reinterpret_cast<const u32x2*>(from);
+                packed[i / 2] = p[0];
+                packed[i / 2 + 1] = p[1];
+            } else {
+                packed[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(from) << (16 * (i & 1));
             }
         }
         if (g >= lead && g + 8 <= lead + total) {
@@ -652,9 +682,8 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
     a.end_token = (uint32_t)total;
     a.side = side;
     a.per_strip = std::max(1u, kStripPixels / side);
-    /* (behind the last row: what the gather reads for places outside the image) */
-    const size_t lds = 768 * 2 + (size_t)((a.per_strip * side * 3 + 3) / 4 * 4) * side + 32;
-    const auto kernel = side % 8 == 0 ? l3_patch_tokens_kernel<8> : side % 4 == 0 ? l3_patch_tokens_kernel<4> : side % 2 == 0 ? l3_patch_tokens_kernel<2> : l3_patch_tokens_kernel<1>;
+    const size_t lds = 768 * 2 + (size_t)a.per_strip * patch_pitch(3 * side * side);
+    const auto kernel = side % 4 == 0 ? l3_patch_tokens_kernel<4, 8> : side % 2 == 0 ? l3_patch_tokens_kernel<2, 4> : l3_patch_tokens_kernel<1, 1>;
     uint32_t first = 0;
     for (int i0 = 0; i0 < n; i0 += (int)kTokenImages) {
         a.images = (uint32_t)std::min<int>((int)kTokenImages, n - i0);
