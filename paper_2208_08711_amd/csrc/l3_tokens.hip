@@ -49,7 +49,7 @@ struct TokenImage {
 
 struct TokenArgs {
     TokenImage image[kTokenImages];
-    uint16_t table[768];                   /* l3_normalized_values */
+    alignas(4) uint16_t table[768];        /* l3_normalized_values */
     uint16_t* tokens;
     int32_t* positions;
     int32_t* first;
@@ -87,12 +87,29 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     const uint32_t count = min(a.per_strip, cols - col0);
     const uint32_t token0 = im.first_token + row * cols + col0;
 
-    for (uint32_t i = tid; i < 768; i += kTokenThreads) table[i] = a.table[i];
     const uint32_t x0 = col0 * side, y0 = row * side;
     const uint32_t width = min(count * side, im.width - x0), height = min(side, im.height - y0);   /* inside the image */
     const uint32_t area = side * side, size = 3 * area, pitch = patch_pitch(size);
     const uint32_t quads = (count * side + 3) / 4, by_quads = reciprocal(quads), by_side = reciprocal(side);
-    const uint8_t* const corner = im.rgb + (uint64_t)y0 * im.row_stride + (uint64_t)x0 * 3;
+    const uint8_t* const line = im.rgb + (uint64_t)y0 * im.row_stride;
+    /* Four pixels' bytes: 12 in one piece, at the end of a row those before it, moved (images of less
+     * than four columns: byte by byte).  Any for what is outside. */
+    const auto bytes_of = [&](uint32_t i) {
+        const uint32_t y = min(quotient(i, quads, by_quads), height - 1), x = x0 + (i - quotient(i, quads, by_quads) * quads) * 4;
+        const uint8_t* const src = line + (uint64_t)y * im.row_stride;
+        if (im.width >= 4) return (u32x3)*reinterpret_cast<const u32x3_any*>(src + 3 * min(x, im.width - 4));
+        u32x3 v = {};
+#pragma unroll
+        for (uint32_t k = 0; k < 9; ++k)
+            if (k < 3 * im.width) v[k / 4] |= (uint32_t)src[k] << (8 * (k % 4));
+        return v;
+    };
+    const uint32_t all = quads * side;
+    /* the first bytes are on the way while the table comes */
+    u32x3 ahead[2];
+#pragma unroll
+    for (uint32_t u = 0; u < 2; ++u) ahead[u] = bytes_of(min(tid + u * kTokenThreads, all - 1));
+    for (uint32_t i = tid; i < 768 / 2; i += kTokenThreads) reinterpret_cast<uint32_t*>(table)[i] = reinterpret_cast<const uint32_t*>(a.table)[i];
     if (a.positions)
         for (uint32_t t = tid; t < count; t += kTokenThreads) {
             int32_t* p = a.positions + 2 * (uint64_t)(token0 + t);
@@ -105,37 +122,43 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
     }
     __syncthreads();
 
-#pragma unroll 2
-    for (uint32_t i = tid; i < quads * side; i += kTokenThreads) {
-        const uint32_t y = quotient(i, quads, by_quads), x = (i - y * quads) * 4;
-        uint32_t v[3] = {};
-        const uint32_t inside = y < height && x < width ? min(4u, width - x) : 0u;    /* pixels */
-        const uint8_t* const src = corner + (uint64_t)y * im.row_stride + 3 * x;
-        if (inside == 4) {
-            const u32x3_any w = *reinterpret_cast<const u32x3_any*>(src);
+    for (uint32_t i0 = tid; i0 < all; i0 += 2 * kTokenThreads) {
+        u32x3 now[2];
 #pragma unroll
-            for (uint32_t k = 0; k < 3; ++k) v[k] = w[k];
-        } else {
+        for (uint32_t u = 0; u < 2; ++u) now[u] = ahead[u];
+        if (i0 + 2 * kTokenThreads < all)
 #pragma unroll
-            for (uint32_t k = 0; k < 9; ++k)
-                if (k < 3 * inside) v[k / 4] |= (uint32_t)src[k] << (8 * (k % 4));
-        }
-        uint32_t value[3][4];
+            for (uint32_t u = 0; u < 2; ++u) ahead[u] = bytes_of(min(i0 + (2 + u) * kTokenThreads, all - 1));
 #pragma unroll
-        for (uint32_t k = 0; k < 12; ++k) {
-            const uint32_t found = table[(k % 3) * 256 + ((v[k / 4] >> (8 * (k % 4))) & 255u)];
-            value[k % 3][k / 3] = k / 3 < inside ? found : 0u;
-        }
+        for (uint32_t u = 0; u < 2; ++u) {
+            const uint32_t i = i0 + u * kTokenThreads;
+            if (i >= all) break;
+            const uint32_t y = quotient(i, quads, by_quads), x = (i - y * quads) * 4;
+            const uint32_t inside = y < height && x < width ? min(4u, width - x) : 0u;    /* pixels */
+            u32x3 v = now[u];
+            if (inside && inside < 4 && im.width >= 4 && x0 + x + 4 > im.width) {
+                const uint32_t skip = 24 * (x0 + x + 4 - im.width);
+                uint64_t low = (uint64_t)v[1] << 32 | v[0], high = v[2];
+                low = skip < 64 ? low >> skip | high << (64 - skip) : high >> (skip - 64);
+                v = u32x3{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)(skip < 64 ? high >> skip : 0u)};
+            }
+            uint32_t value[3][4];
 #pragma unroll
-        for (uint32_t k = 0; k < 4; k += RUN) {
-            const uint32_t t = quotient(x + k, side, by_side);
-            if (RUN < 4 && t >= count) break;
-            uint8_t* const to = patches + t * pitch + 2 * (y * side + (x + k - t * side));
+            for (uint32_t k = 0; k < 12; ++k) {
+                const uint32_t found = table[(k % 3) * 256 + ((v[k / 4] >> (8 * (k % 4))) & 255u)];
+                value[k % 3][k / 3] = k / 3 < inside ? found : 0u;
+            }
 #pragma unroll
-            for (uint32_t c = 0; c < 3; ++c) {
-                if (RUN == 4) *reinterpret_cast<u32x2*>(to + 2 * c * area) = u32x2{value[c][0] | value[c][1] << 16, value[c][2] | value[c][3] << 16};
-                else if (RUN == 2) *reinterpret_cast<uint32_t*>(to + 2 * c * area) = value[c][k] | value[c][k + 1] << 16;
-                else *reinterpret_cast<uint16_t*>(to + 2 * c * area) = (uint16_t)value[c][k];
+            for (uint32_t k = 0; k < 4; k += RUN) {
+                const uint32_t t = quotient(x + k, side, by_side);
+                if (RUN < 4 && t >= count) break;
+                uint8_t* const to = patches + t * pitch + 2 * (y * side + (x + k - t * side));
+#pragma unroll
+                for (uint32_t c = 0; c < 3; ++c) {
+                    if (RUN == 4) *reinterpret_cast<u32x2*>(to + 2 * c * area) = u32x2{value[c][0] | value[c][1] << 16, value[c][2] | value[c][3] << 16};
+                    else if (RUN == 2) *reinterpret_cast<uint32_t*>(to + 2 * c * area) = value[c][k] | value[c][k + 1] << 16;
+                    else *reinterpret_cast<uint16_t*>(to + 2 * c * area) = (uint16_t)value[c][k];
+                }
             }
         }
     }
