@@ -24,8 +24,7 @@ bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) 
  * Patch tokens
  * ------------------------------------------------------------------------ */
 
-/* A workgroup takes a strip: up to kStripPixels pixels' width of consecutive patches of one patch
- * row of one image, whose tokens lie end to end in the output.  A lane takes four pixels (12 bytes) of a row,
+/* A workgroup takes a strip: up to kStripBytes of output, consecutive patches of one patch row of one image, whose tokens lie end to end in the output.  A lane takes four pixels (12 bytes) of a row,
  * looks the values of their bytes up and puts them, channel by channel, where they belong in an image of the
  * output in local memory, RUN pixels of a patch's row at a time; from there whole lines go out, PIECE
  * elements at a time (a patch is a multiple of that).  RUN, PIECE: 4, 8 where 4 divides the side, 2, 4
@@ -36,7 +35,7 @@ typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
 typedef u32x3 u32x3_any __attribute__((aligned(1)));
 
 constexpr int kTokenThreads = 256;
-constexpr uint32_t kStripPixels = 128;
+constexpr uint32_t kStripBytes = 24576;
 constexpr uint32_t kTokenImages = 64;      /* descriptors in the arguments of one launch */
 
 struct TokenImage {
@@ -145,8 +144,12 @@ __global__ __launch_bounds__(kTokenThreads) void l3_patch_tokens_kernel(TokenArg
             uint32_t value[3][4];
 #pragma unroll
             for (uint32_t k = 0; k < 12; ++k) {
-                const uint32_t found = table[(k % 3) * 256 + ((v[k / 4] >> (8 * (k % 4))) & 255u)];
-                value[k % 3][k / 3] = k / 3 < inside ? found : 0u;
+                value[k % 3][k / 3] = table[(k % 3) * 256 + ((v[k / 4] >> (8 * (k % 4))) & 255u)];
+            }
+            if (inside < 4) {
+#pragma unroll
+                for (uint32_t k = 0; k < 12; ++k)
+                    if (k / 3 >= inside) value[k % 3][k / 3] = 0;
             }
 #pragma unroll
             for (uint32_t k = 0; k < 4; k += RUN) {
@@ -704,7 +707,7 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
     a.all_images = (uint32_t)n;
     a.end_token = (uint32_t)total;
     a.side = side;
-    a.per_strip = std::max(1u, kStripPixels / side);
+    a.per_strip = std::max(1u, kStripBytes / patch_pitch(3 * side * side));
     const size_t lds = 768 * 2 + (size_t)a.per_strip * patch_pitch(3 * side * side);
     const auto kernel = side % 4 == 0 ? l3_patch_tokens_kernel<4, 8> : side % 2 == 0 ? l3_patch_tokens_kernel<2, 4> : l3_patch_tokens_kernel<1, 1>;
     uint32_t first = 0;
