@@ -415,53 +415,72 @@ MAX_PATCH_SIDE, MAX_HEAD_DIM = 64, 128
 _NORM_ROTATE_WORKSPACE = 1024 * 2 * 128 * 4
 
 
-def _half(*tensors):
-    """The l3_dtype that all the tensors have."""
+# (Small calls are host work for the most part, 10 us of it for 3 us of kernel when every check asked
+# torch anew: torch's types and its lookup of the current stream are kept, and a tensor is asked for what is
+# needed once.)
+_torch = _half_types = _raw_stream = None
+
+
+def _load_torch():
+    global _torch, _half_types, _raw_stream
     import torch
-    kind = {torch.bfloat16: BF16, torch.float16: FP16}.get(tensors[0].dtype)
-    if kind is None or any(t.dtype != tensors[0].dtype for t in tensors):
-        raise ValueError("expected bfloat16 or float16 tensors of one type")
-    return kind
+    _half_types = {torch.bfloat16: BF16, torch.float16: FP16}
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _torch = torch
 
 
-def _on_gpu(*tensors):
-    device = None
+def _common(tensors, others=()):
+    """(l3_dtype, index of the GPU) that all the tensors have; others, which may be None: of the GPU only."""
+    if _torch is None:
+        _load_torch()
+    dtype, index = tensors[0].dtype, tensors[0].get_device()
+    kind = _half_types.get(dtype)
+    if kind is None:
+        raise ValueError("expected bfloat16 or float16 tensors")
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or (device is not None and t.device != device):
+        if t.dtype is not dtype:
+            raise ValueError("expected tensors of one type")
+        if t.get_device() != index:
             raise ValueError("expected tensors of one GPU")
-        device = t.device
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError("expected tensors of one GPU")
+    if index < 0:
+        raise ValueError("expected tensors of one GPU")
+    return kind, index
+
+
+def _stream_on(index, stream):
+    return _raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def _words(t, kind, count, what):
     """Address of a contiguous device tensor of `count` elements of a type (None: 0)."""
     if t is None:
         return None
-    if str(t.dtype) != "torch." + kind or not t.is_contiguous() or t.numel() != count:
+    if t.dtype is not getattr(_torch, kind) or t.numel() != count or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor of %d elements" % (what, kind, count))
     return t.data_ptr()
 
 
-def _heads(t, tokens=None, heads=None, head_dim=None):
-    """l3_heads of a [tokens, heads, head_dim] tensor."""
-    shape = tuple(t.shape)
-    if t.dim() != 3 or any(w is not None and w != s for w, s in zip((tokens, heads, head_dim), shape)):
-        raise ValueError("expected [tokens, heads, head_dim] = %s, got %s" % ((tokens, heads, head_dim), shape))
-    if t.stride(2) != 1 and shape[2] > 1 and t.numel():
+def _heads(t, shape):
+    """l3_heads of a [tokens, heads, head_dim] tensor of the shape given."""
+    if t.shape != shape or len(shape) != 3:
+        raise ValueError("expected [tokens, heads, head_dim] = %s, got %s" % (tuple(shape), tuple(t.shape)))
+    token, head, element = t.stride()
+    if element != 1 and shape[2] > 1 and t.numel():
         raise ValueError("the elements of a head must lie side by side")
     # (a dimension of one has no stride to speak of)
-    return _Heads(t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else 0)
+    return _Heads(t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
 def _workspace(given, size, like, stream):
     """The caller's workspace, or one of torch's that lives as long as the stream needs it."""
-    import torch
     if given is not None:
-        if not given.is_cuda or not given.is_contiguous():
-            raise ValueError("workspace: expected a contiguous device tensor")
+        if given.get_device() != like.get_device() or not given.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the GPU of the others")
         return given, given.numel() * given.element_size()
-    given = torch.empty(max(size, 16), dtype=torch.uint8, device=like.device)
+    given = _torch.empty(max(size, 16), dtype=_torch.uint8, device=like.device)
     if stream is not None:
         given.record_stream(stream)
     return given, given.numel()
@@ -476,24 +495,24 @@ def patch_tokens_batch(ctx, images, side, mean, stdv, tokens, positions=None, fi
     strides say otherwise or row_strides is given); tokens: device tensor [total, 3*side*side]; positions: int32
     [total, 2] or None; first: int32 [len(images) + 1] or None.  Enqueues on `stream` (default: torch's current)."""
     n = len(images)
+    kind, index = _common([tokens], (positions, first, *images))
     arr = (_TokenImage * max(n, 1))()
     for i, image in enumerate(images):
-        if str(image.dtype) != "torch.uint8" or image.dim() != 3 or image.shape[2] != 3 or image.stride(2) != 1 or image.stride(1) != 3:
+        if image.dtype is not _torch.uint8 or image.dim() != 3 or image.shape[2] != 3 or image.stride(2) != 1 or image.stride(1) != 3:
             raise ValueError("expected uint8 [H, W, 3] with pixels side by side")
         arr[i].d_rgb, arr[i].height, arr[i].width = image.data_ptr(), image.shape[0], image.shape[1]
         arr[i].row_stride = max(image.stride(0), 3 * image.shape[1]) if row_strides is None else row_strides[i]
-    _on_gpu(tokens, positions, first, *images)
     if tokens.dim() != 2 or not tokens.is_contiguous() or tokens.shape[1] != 3 * side * side:
         raise ValueError("tokens: expected a contiguous [total, 3*side*side]")
     m, s = (ctypes.c_float * 3)(*mean), (ctypes.c_float * 3)(*stdv)
     _check(_load().l3_patch_tokens_batch(
-        ctx.handle, arr, n, side, m, s, _half(tokens), tokens.data_ptr(), tokens.shape[0],
-        _words(positions, "int32", 2 * tokens.shape[0], "positions"), _words(first, "int32", n + 1, "first"), _stream_ptr(stream)),
+        ctx.handle, arr, n, side, m, s, kind, tokens.data_ptr(), tokens.shape[0],
+        _words(positions, "int32", 2 * tokens.shape[0], "positions"), _words(first, "int32", n + 1, "first"), _stream_on(index, stream)),
         "l3_patch_tokens_batch")
 
 
 def _rows(t, shape):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("expected a tensor of shape %s, got %s" % (tuple(shape), tuple(t.shape)))
     if t.dim() != 2:
         if not t.is_contiguous():
@@ -508,8 +527,7 @@ def dropout(ctx, x, out, p, seed, offset=0, residual=None, device_offset=None, s
     """out = (residual +) x with a share p of the elements dropped and the others scaled up.  [rows, cols] with any row
     stride, or contiguous of any shape.  The gradient: the same call on the gradient, without residual.
     device_offset: int64 (or uint64) device tensor of one word, added to offset when the kernel runs."""
-    _on_gpu(x, out, residual, device_offset)
-    kind = _half(*(t for t in (x, out, residual) if t is not None))
+    kind, index = _common((x, out) if residual is None else (x, out, residual), (device_offset,))
     strides = [0 if t is None else _rows(t, x.shape) for t in (x, residual, out)]
     if device_offset is not None and (device_offset.numel() != 1 or device_offset.element_size() != 8):
         raise ValueError("device_offset: expected one 64-bit word")
@@ -518,7 +536,7 @@ def dropout(ctx, x, out, p, seed, offset=0, residual=None, device_offset=None, s
     _check(_load().l3_dropout(
         ctx.handle, x.data_ptr(), strides[0], None if residual is None else residual.data_ptr(), strides[1], out.data_ptr(), strides[2],
         rows, cols, kind, float(p), int(seed) & _MASK64, int(offset) & _MASK64,
-        None if device_offset is None else device_offset.data_ptr(), _stream_ptr(stream)), "l3_dropout")
+        None if device_offset is None else device_offset.data_ptr(), _stream_on(index, stream)), "l3_dropout")
 
 
 def rotation_turns(pairs, base=10000.0, factor=1.0, original_length=0.0, slow=1.0, fast=32.0):
@@ -546,57 +564,61 @@ class Rotation:
         return ctypes.byref(_Rotation(self.pairs, self.axes, self.interleaved, self.magnitude, self.turns, where))
 
 
+_NO_HEADS = _Heads()
+
+
 def _side(tokens, head_dim, *tensors):
     """(heads, l3_heads of each) of tensors of one shape; nothing where the first is None."""
-    if tensors[0] is None:
-        return 0, [_Heads() for _ in tensors]
-    return tensors[0].shape[1], [_heads(t, tokens, tensors[0].shape[1], head_dim) for t in tensors]
+    shape = tensors[0].shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != head_dim:
+        raise ValueError("expected [tokens, heads, head_dim] = (%d, ?, %d), got %s" % (tokens, head_dim, tuple(shape)))
+    return shape[1], [_heads(t, shape) for t in tensors]
 
 
 def rotate(ctx, rotation, positions, q, q_out, k=None, k_out=None, inverse=False, stream=None):
     """Queries and keys (or one tensor alone) [tokens, heads, head_dim] turned by their positions, int32 [tokens] or
     [tokens, axes].  inverse=True turns back, which is also the gradients' way."""
-    tensors = [t for t in (q, q_out, k, k_out) if t is not None]
-    _on_gpu(positions, *tensors)
-    tokens, head_dim = q.shape[0], q.shape[2]
+    kind, index = _common((q, q_out) if k is None else (q, q_out, k, k_out), (positions,))
+    tokens, head_dim = q.shape[0], q.shape[-1]
     hq, (a, b) = _side(tokens, head_dim, q, q_out)
-    hk, (c, d) = _side(tokens, head_dim, k, k_out)
-    _check(_load().l3_rotate(ctx.handle, rotation._with(positions, tokens), int(bool(inverse)), tokens, head_dim, hq, a, b, hk, c, d,
-                             _half(*tensors), _stream_ptr(stream)), "l3_rotate")
+    hk, (c, d) = _side(tokens, head_dim, k, k_out) if k is not None else (0, (_NO_HEADS, _NO_HEADS))
+    _check(_load().l3_rotate(ctx.handle, rotation._with(positions, tokens), 1 if inverse else 0, tokens, head_dim, hq, a, b, hk, c, d,
+                             kind, _stream_on(index, stream)), "l3_rotate")
 
 
 def norm_rotate(ctx, rotation, positions, q, q_weight, q_out, k=None, k_weight=None, k_out=None, eps=1e-6, stream=None):
     """Every head of the queries and keys normalised, weighted (float32 [head_dim]) and turned."""
-    tensors = [t for t in (q, q_out, k, k_out) if t is not None]
-    _on_gpu(positions, q_weight, k_weight, *tensors)
-    tokens, head_dim = q.shape[0], q.shape[2]
+    kind, index = _common((q, q_out) if k is None else (q, q_out, k, k_out), (positions, q_weight, k_weight))
+    tokens, head_dim = q.shape[0], q.shape[-1]
     hq, (a, b) = _side(tokens, head_dim, q, q_out)
-    hk, (c, d) = _side(tokens, head_dim, k, k_out)
+    hk, (c, d) = _side(tokens, head_dim, k, k_out) if k is not None else (0, (_NO_HEADS, _NO_HEADS))
     _check(_load().l3_norm_rotate(
         ctx.handle, rotation._with(positions, tokens), float(eps), tokens, head_dim,
         hq, a, _words(q_weight, "float32", head_dim, "q_weight"), b, hk, c, _words(k_weight, "float32", head_dim, "k_weight"), d,
-        _half(*tensors), _stream_ptr(stream)), "l3_norm_rotate")
+        kind, _stream_on(index, stream)), "l3_norm_rotate")
 
 
 def norm_rotate_backward(ctx, rotation, positions, q, q_weight, q_grad, q_back, q_weight_grad,
                          k=None, k_weight=None, k_grad=None, k_back=None, k_weight_grad=None, eps=1e-6, workspace=None, stream=None):
     """Gradients of norm_rotate: q_grad, k_grad are those of its outputs, q_back, k_back and the weights'
     (float32 [head_dim]) are written."""
-    tensors = [t for t in (q, q_grad, q_back, k, k_grad, k_back) if t is not None]
-    _on_gpu(positions, q_weight, k_weight, q_weight_grad, k_weight_grad, *tensors)
-    tokens, head_dim = q.shape[0], q.shape[2]
+    kind, index = _common((q, q_grad, q_back) if k is None else (q, q_grad, q_back, k, k_grad, k_back),
+                          (positions, q_weight, k_weight, q_weight_grad, k_weight_grad))
+    tokens, head_dim = q.shape[0], q.shape[-1]
     hq, (a, b, c) = _side(tokens, head_dim, q, q_grad, q_back)
-    hk, (d, e, f) = _side(tokens, head_dim, k, k_grad, k_back)
+    hk, (d, e, f) = _side(tokens, head_dim, k, k_grad, k_back) if k is not None else (0, (_NO_HEADS,) * 3)
     room, size = _workspace(workspace, _NORM_ROTATE_WORKSPACE, q, stream)
     _check(_load().l3_norm_rotate_backward(
         ctx.handle, rotation._with(positions, tokens), float(eps), tokens, head_dim,
         hq, a, _words(q_weight, "float32", head_dim, "q_weight"), b, c, _words(q_weight_grad, "float32", head_dim, "q_weight_grad"),
         hk, d, _words(k_weight, "float32", head_dim, "k_weight"), e, f, _words(k_weight_grad, "float32", head_dim, "k_weight_grad"),
-        _half(*tensors), room.data_ptr(), size, _stream_ptr(stream)), "l3_norm_rotate_backward")
+        kind, room.data_ptr(), size, _stream_on(index, stream)), "l3_norm_rotate_backward")
 
 
 def _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, kind):
     images = q_first.numel() - 1
+    if q.dim() != 3 or k.dim() != 3 or k.shape[2] != q.shape[2]:
+        raise ValueError("expected queries and keys [tokens, heads, head_dim] of one head_dim")
     if kv_first is None and k.shape[0] != q.shape[0]:
         raise ValueError("kv_first: queries and keys differ in number")
     head_dim = q.shape[2]
@@ -611,32 +633,32 @@ def attention(ctx, q, k, v, out, q_first, kv_first=None, mask=MASK_DOCUMENT, pre
     """q, out: [tokens, q_heads, head_dim]; k, v: [kv_tokens, kv_heads, head_dim]; q_first (and kv_first): int32
     [images + 1]; prefix: int32 [images]; slopes: float32 [q_heads]; lse: float32 [q_heads, tokens] for the
     gradients.  scale: default head_dim ** -0.5."""
-    _on_gpu(q, k, v, out, q_first, kv_first, prefix, slopes, lse)
-    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, _half(q, k, v, out))
+    kind, index = _common((q, k, v, out), (q_first, kv_first, prefix, slopes, lse))
+    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, kind)
     _check(_load().l3_attention(
-        ctx.handle, ctypes.byref(shape), _heads(q), _heads(k, None, None, q.shape[2]), _heads(v, *k.shape), _heads(out, *q.shape),
-        _words(lse, "float32", q.shape[0] * q.shape[1], "lse"), _stream_ptr(stream)), "l3_attention")
+        ctx.handle, ctypes.byref(shape), _heads(q, q.shape), _heads(k, k.shape), _heads(v, k.shape), _heads(out, q.shape),
+        _words(lse, "float32", q.shape[0] * q.shape[1], "lse"), _stream_on(index, stream)), "l3_attention")
 
 
 def attention_backward(ctx, q, k, v, out, lse, out_grad, q_grad, k_grad, v_grad, q_first, kv_first=None, mask=MASK_DOCUMENT, prefix=None,
                        scale=None, cap=0.0, slopes=None, workspace=None, stream=None):
     """Gradients of attention(): q_grad, k_grad and v_grad are written."""
-    _on_gpu(q, k, v, out, lse, out_grad, q_grad, k_grad, v_grad, q_first, kv_first, prefix, slopes)
-    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes,
-                             _half(q, k, v, out, out_grad, q_grad, k_grad, v_grad))
+    kind, index = _common((q, k, v, out, out_grad, q_grad, k_grad, v_grad), (lse, q_first, kv_first, prefix, slopes))
+    shape = _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, kind)
     lib = _load()
     room, size = _workspace(workspace, lib.l3_attention_workspace(ctypes.byref(shape)), q, stream)
+    of_q, of_k = q.shape, k.shape
     _check(lib.l3_attention_backward(
-        ctx.handle, ctypes.byref(shape), _heads(q), _heads(k, None, None, q.shape[2]), _heads(v, *k.shape), _heads(out, *q.shape),
-        _words(lse, "float32", q.shape[0] * q.shape[1], "lse"), _heads(out_grad, *q.shape), _heads(q_grad, *q.shape),
-        _heads(k_grad, *k.shape), _heads(v_grad, *k.shape), room.data_ptr(), size, _stream_ptr(stream)), "l3_attention_backward")
+        ctx.handle, ctypes.byref(shape), _heads(q, of_q), _heads(k, of_k), _heads(v, of_k), _heads(out, of_q),
+        _words(lse, "float32", of_q[0] * of_q[1], "lse"), _heads(out_grad, of_q), _heads(q_grad, of_q),
+        _heads(k_grad, of_k), _heads(v_grad, of_k), room.data_ptr(), size, _stream_on(index, stream)), "l3_attention_backward")
 
 
 def attention_step(ctx, q, k_cache, v_cache, lengths, out, scale=None, cap=0.0, slopes=None, max_length=None, workspace=None, stream=None):
     """One query a sequence: q, out [n, q_heads, head_dim]; caches [n, room, kv_heads, head_dim]; lengths int32 [n];
     max_length: what no length exceeds (default: the caches' room)."""
-    _on_gpu(q, k_cache, v_cache, lengths, out, slopes)
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or k_cache.shape[0] != q.shape[0]:
+    kind, index = _common((q, k_cache, v_cache, out), (lengths, slopes))
+    if q.dim() != 3 or k_cache.dim() != 4 or v_cache.shape != k_cache.shape or k_cache.shape[0] != q.shape[0]:
         raise ValueError("expected caches [n, room, kv_heads, head_dim]")
     n, hq, head_dim = q.shape
     room_for = k_cache.shape[1]
@@ -653,6 +675,6 @@ def attention_step(ctx, q, k_cache, v_cache, lengths, out, scale=None, cap=0.0, 
     lib = _load()
     room, size = _workspace(workspace, lib.l3_attention_step_workspace(n, head_dim, hq, k_cache.shape[2], most), q, stream)
     _check(lib.l3_attention_step(
-        ctx.handle, n, head_dim, hq, k_cache.shape[2], _heads(q), *caches, _words(lengths, "int32", n, "lengths"), most,
-        head_dim ** -0.5 if scale is None else float(scale), float(cap), _words(slopes, "float32", hq, "slopes"), _heads(out, *q.shape),
-        _half(q, k_cache, v_cache, out), room.data_ptr(), size, _stream_ptr(stream)), "l3_attention_step")
+        ctx.handle, n, head_dim, hq, k_cache.shape[2], _heads(q, q.shape), *caches, _words(lengths, "int32", n, "lengths"), most,
+        head_dim ** -0.5 if scale is None else float(scale), float(cap), _words(slopes, "float32", hq, "slopes"), _heads(out, q.shape),
+        kind, room.data_ptr(), size, _stream_on(index, stream)), "l3_attention_step")
