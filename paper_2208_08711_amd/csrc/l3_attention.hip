@@ -820,6 +820,7 @@ __global__ __launch_bounds__(kThreads) void l3_attention_kv_join_kernel(Backward
 
 constexpr int kStepKeys = 32;              /* of a wave's tile */
 constexpr int kStepWaves = 2, kStepThreads = 64 * kStepWaves;
+constexpr int kStepGrid = 8192;            /* workgroups wanted of a launch, if all caches were full */
 constexpr int kStepRecord = 2;             /* floats of a partial result ahead of its head_dim: top, sum */
 
 struct StepArgs {
@@ -840,12 +841,13 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
     constexpr int kTile = kStepKeys * Tile<DB>::kPitch;
     extern __shared__ __attribute__((aligned(256))) uint8_t step_lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    /* heads side by side in memory are read side by side in time */
     int at = blockIdx.x;
-    const int chunk = at % a.chunks;
-    at /= a.chunks;
+    const int kv_head = at % a.kv_heads;
+    at /= a.kv_heads;
     const int of = at % a.blocks_of_heads;
     at /= a.blocks_of_heads;
-    const int kv_head = at % a.kv_heads, sequence = at / a.kv_heads;
+    const int chunk = at % a.chunks, sequence = at / a.chunks;
     const int length = __builtin_amdgcn_readfirstlane(min(max(a.lengths[sequence], 0), a.max_length));
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, length);
     const int in_group = of * 32 + (lane & 31), head = kv_head * a.group + in_group;
@@ -933,13 +935,28 @@ __global__ __launch_bounds__(L3_MAX_HEAD_DIM) void l3_attention_join_kernel(Step
     if (c >= a.head_dim) return;
     const int64_t pitch = a.head_dim + kStepRecord;
     const float* const record = a.partial + ((int64_t)sequence * a.q_heads + head) * a.chunks * pitch;
-    float top = -kInf;
-    for (int i = 0; i < chunks; ++i) top = fmaxf(top, record[i * pitch]);
-    float total = 0.0f, x = 0.0f;
-    for (int i = 0; i < chunks; ++i) {
-        const float f = record[i * pitch] > -kInf ? __builtin_amdgcn_exp2f(record[i * pitch] - top) : 0.0f;
-        total += f * record[i * pitch + 1];
-        x += f * record[i * pitch + kStepRecord + c];
+    /* four chunks at a time, so that their loads travel together */
+    float top = -kInf, total = 0.0f, x = 0.0f;
+    for (int i = 0; i < chunks; i += 4) {
+        float tops[4], sums[4], parts[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float* const r = record + min(i + k, chunks - 1) * pitch;
+            tops[k] = i + k < chunks ? r[0] : -kInf;
+            sums[k] = r[1];
+            parts[k] = r[kStepRecord + c];
+        }
+        const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), next = fmaxf(top, most);
+        const float shrink = top > -kInf ? __builtin_amdgcn_exp2f(top - next) : 0.0f;
+        total *= shrink;
+        x *= shrink;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = tops[k] > -kInf ? __builtin_amdgcn_exp2f(tops[k] - next) : 0.0f;
+            total = __builtin_fmaf(f, sums[k], total);
+            x = __builtin_fmaf(f, parts[k], x);
+        }
+        top = next;
     }
     ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + (int64_t)head * a.out.head + c] = (T)(chunks > 0 ? x / total : 0.0f);
 }
@@ -1054,7 +1071,7 @@ l3_status run_backward(const BackwardArgs& a, hipStream_t stream) {
 /* How the caches are cut: chunks of whole rounds of the waves, so many that every CU has a few
  * workgroups, and none so short that joining them would cost more than it gives. */
 void plan_step(int n, int kv_heads, int blocks_of_heads, int64_t max_length, int32_t* chunk, int32_t* chunks) {
-    const int64_t rows = (int64_t)n * kv_heads * blocks_of_heads, wanted = std::max<int64_t>(1, 2048 / rows), round = kStepWaves * kStepKeys;
+    const int64_t rows = (int64_t)n * kv_heads * blocks_of_heads, wanted = std::max<int64_t>(1, kStepGrid / rows), round = kStepWaves * kStepKeys;
     const int64_t each = std::max<int64_t>(4 * round, ((max_length + wanted - 1) / wanted + round - 1) / round * round);
     *chunk = (int32_t)std::min<int64_t>(each, (int64_t)1 << 30);
     *chunks = (int32_t)std::max<int64_t>(1, (max_length + *chunk - 1) / *chunk);
