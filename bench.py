@@ -284,6 +284,54 @@ def measure_encode(torch, l3, ctx, images, files, stream, patch):
                     "works the offsets out, and calls of few strips take one"}
 
 
+def measure_tokens(torch, l3, ctx, images, stream):
+    """The decoded images as packed 16x16 patch tokens (bf16), and what one block of a model that trains on
+    them computes next to its matrix products: dropout on 768 columns, queries and keys of 12 heads of 64 normalised
+    and turned, attention inside each image and all their gradients; each for itself, on this workload's images."""
+    from paper_2208_08711_amd import synth
+    side, width, heads, dim = 16, 768, 12, 64
+    pixels = [torch.from_numpy(np.ascontiguousarray(im)).cuda() for im in images]
+    counts = [l3.patch_tokens_count(im.shape[1], im.shape[0], side) for im in images]
+    total = sum(counts)
+    bf16 = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_()
+    tokens = bf16(total, 3 * side * side)
+    positions = torch.empty((total, 2), dtype=torch.int32, device="cuda")
+    first = torch.empty(len(images) + 1, dtype=torch.int32, device="cuda")
+    x, joint, grad = bf16(total, width), bf16(total, 3 * heads, dim), bf16(total, heads, dim)
+    q, k, v = joint[:, :heads], joint[:, heads:2 * heads], joint[:, 2 * heads:]
+    qn, kn, out, qg, kg = (torch.empty_like(grad) for _ in range(5))
+    joint_grad = torch.empty_like(joint)
+    lse = torch.empty((heads, total), device="cuda")
+    weights = [torch.ones(dim, device="cuda") for _ in range(4)]
+    rotation = l3.Rotation(l3.rotation_turns(dim // 4) * 2, axes=2)
+    calls = (
+        ("patch_tokens", lambda: l3.patch_tokens_batch(ctx, pixels, side, synth.IMAGENET_MEAN, synth.IMAGENET_STD, tokens, positions=positions,
+                                                       first=first, stream=stream)),
+        ("dropout", lambda: l3.dropout(ctx, x, x, 0.1, 1, stream=stream)),
+        ("norm_rotate", lambda: l3.norm_rotate(ctx, rotation, positions, q, weights[0], qn, k, weights[1], kn, stream=stream)),
+        ("attention", lambda: l3.attention(ctx, qn, kn, v, out, first, lse=lse, stream=stream)),
+        ("attention_backward", lambda: l3.attention_backward(ctx, qn, kn, v, out, lse, grad, qg, kg, joint_grad[:, 2 * heads:], first, stream=stream)),
+        ("norm_rotate_backward", lambda: l3.norm_rotate_backward(
+            ctx, rotation, positions, q, weights[0], qg, joint_grad[:, :heads], weights[2], k, weights[1], kg,
+            joint_grad[:, heads:2 * heads], weights[3], stream=stream)))
+    products = 2 * dim * heads * sum(c * c for c in counts)          # operations of one product of the attention
+    result = {"tokens": total, "images": len(images), "heads": heads, "head_dim": dim, "dtype": "bf16"}
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for name, call in calls:
+        call()
+        torch.cuda.synchronize()
+        e0.record(stream)
+        for _ in range(10):
+            call()
+        e1.record(stream)
+        torch.cuda.synchronize()
+        ms = e0.elapsed_time(e1) / 10
+        result[name + "_ms"] = ms
+        if name.startswith("attention"):
+            result[name + "_tflops"] = products * (2 if name == "attention" else 5) / (ms * 1e-3) / 1e12
+    return result
+
+
 def measure_overlap(torch, step, stream, steps, decode_alone_ms):
     """Decode steps on `stream`, a bf16 GEMM loop on a second stream (both default priority):
     each alone, and the rates of both while both streams have work.  The decode steps are
@@ -373,6 +421,9 @@ def main():
     ap.add_argument("--encode", action="store_true",
                     help="also time l3_encode_batch on the same images (pixels resident in HBM) "
                          "and check its files against l3_encode_cpu's")
+    ap.add_argument("--tokens", action="store_true",
+                    help="also time the images as packed patch tokens, and the operators of a model "
+                         "that trains on them (include/l3_tokens.h)")
     ap.add_argument("--overlap-gemm", action="store_true",
                     help="also time the decode steps while a bf16 GEMM loop runs on a second "
                          "stream of default priority (Section 4.4 of the paper: decode beside "
@@ -592,6 +643,9 @@ def main():
                                               args.patch, result["roofline"]["launch_ms"])
     if args.encode:
         result["encode"] = measure_encode(torch, l3, ctx, images, files, stream, args.patch)
+
+    if args.tokens:
+        result["tokens"] = measure_tokens(torch, l3, ctx, images, stream)
 
     if not args.no_cpu_baseline:
         import oracle                  # the only use of the oracle here: the reported CPU baseline

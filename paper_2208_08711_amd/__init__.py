@@ -10,5 +10,5 @@ from .binding import (  # noqa: F401
     LAYOUT_HWC, LAYOUT_CHW, BF16, FP16, EXPORTED_SYMBOLS, NOALLOC_MAX_IMAGES,
     ablation_decode_batch, ABLATION_PIXEL_BD, ABLATION_CUSTOM_FILTER, ABLATION_SERIAL_PATCHES, ABLATION_DIAGONAL,
     patch_tokens_count, patch_tokens_batch, dropout, rotation_turns, Rotation, rotate, norm_rotate, norm_rotate_backward,
-    attention, attention_backward, attention_step, MASK_DOCUMENT, MASK_CAUSAL, MASK_PREFIX, MAX_PATCH_SIDE, MAX_HEAD_DIM,
+    attention, attention_backward, attention_step, attention_workspace, attention_step_workspace, NORM_ROTATE_WORKSPACE, MASK_DOCUMENT, MASK_CAUSAL, MASK_PREFIX, MAX_PATCH_SIDE, MAX_HEAD_DIM,
 )

@@ -412,7 +412,7 @@ def encode_batch(ctx, images, files, file_len, patch=0, status=None, stream=None
 
 MASK_DOCUMENT, MASK_CAUSAL, MASK_PREFIX = 0, 1, 2
 MAX_PATCH_SIDE, MAX_HEAD_DIM = 64, 128
-_NORM_ROTATE_WORKSPACE = 1024 * 2 * 128 * 4
+NORM_ROTATE_WORKSPACE = 1024 * 2 * 128 * 4
 
 
 # (Small calls are host work for the most part, 10 us of it for 3 us of kernel when every check asked
@@ -607,7 +607,7 @@ def norm_rotate_backward(ctx, rotation, positions, q, q_weight, q_grad, q_back, 
     tokens, head_dim = q.shape[0], q.shape[-1]
     hq, (a, b, c) = _side(tokens, head_dim, q, q_grad, q_back)
     hk, (d, e, f) = _side(tokens, head_dim, k, k_grad, k_back) if k is not None else (0, (_NO_HEADS,) * 3)
-    room, size = _workspace(workspace, _NORM_ROTATE_WORKSPACE, q, stream)
+    room, size = _workspace(workspace, NORM_ROTATE_WORKSPACE, q, stream)
     _check(_load().l3_norm_rotate_backward(
         ctx.handle, rotation._with(positions, tokens), float(eps), tokens, head_dim,
         hq, a, _words(q_weight, "float32", head_dim, "q_weight"), b, c, _words(q_weight_grad, "float32", head_dim, "q_weight_grad"),
@@ -619,6 +619,8 @@ def _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, 
     images = q_first.numel() - 1
     if q.dim() != 3 or k.dim() != 3 or k.shape[2] != q.shape[2]:
         raise ValueError("expected queries and keys [tokens, heads, head_dim] of one head_dim")
+    if images < 0:
+        raise ValueError("q_first: expected images + 1 elements")
     if kv_first is None and k.shape[0] != q.shape[0]:
         raise ValueError("kv_first: queries and keys differ in number")
     head_dim = q.shape[2]
@@ -626,6 +628,23 @@ def _attention_shape(q, k, q_first, kv_first, mask, prefix, scale, cap, slopes, 
         head_dim, q.shape[1], k.shape[1], images, q.shape[0], k.shape[0], _words(q_first, "int32", images + 1, "q_first"),
         _words(kv_first, "int32", images + 1, "kv_first"), int(mask), _words(prefix, "int32", images, "prefix"),
         head_dim ** -0.5 if scale is None else float(scale), float(cap), _words(slopes, "float32", q.shape[1], "slopes"), kind)
+
+
+def attention_workspace(images, q_tokens, kv_tokens, q_heads, kv_heads, head_dim):
+    """Bytes of attention_backward's workspace."""
+    shape = _AttentionShape(head_dim, q_heads, kv_heads, images, q_tokens, kv_tokens, 16, 16, MASK_DOCUMENT, None, 1.0, 0.0, None, BF16)
+    size = int(_load().l3_attention_workspace(ctypes.byref(shape)))
+    if not size:
+        raise ValueError("l3_attention_workspace refuses these sizes")
+    return size
+
+
+def attention_step_workspace(n, head_dim, q_heads, kv_heads, max_length):
+    """Bytes of attention_step's workspace."""
+    size = int(_load().l3_attention_step_workspace(n, head_dim, q_heads, kv_heads, max_length))
+    if not size:
+        raise ValueError("l3_attention_step_workspace refuses these sizes")
+    return size
 
 
 def attention(ctx, q, k, v, out, q_first, kv_first=None, mask=MASK_DOCUMENT, prefix=None, scale=None, cap=0.0, slopes=None, lse=None,

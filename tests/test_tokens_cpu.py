@@ -232,6 +232,14 @@ def test_step_refusals(lib):
         assert lib.l3_attention_step_workspace(*args) == 0
 
 
+def test_binding_workspaces(lib):
+    assert l3.attention_workspace(3, 100, 100, 4, 2, 64) == lib.l3_attention_workspace(ctypes.byref(shape()))
+    assert l3.attention_step_workspace(3, 64, 4, 2, 1000) == lib.l3_attention_step_workspace(3, 64, 4, 2, 1000) > 0
+    for call in (lambda: l3.attention_workspace(3, 100, 100, 4, 3, 64), lambda: l3.attention_step_workspace(3, 60, 4, 2, 10)):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_binding_checks_tensors():
     """What the library cannot see, the binding checks: types, shapes, devices (here: that they are on a GPU)."""
     half, single = torch.zeros((4, 2, 64), dtype=torch.float16), torch.zeros((4, 2, 64))
