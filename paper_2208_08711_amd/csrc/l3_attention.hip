@@ -302,6 +302,7 @@ __device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVe
         for (int d = 0; d < 2 * DB; ++d) s[b] = mfma(read_row<T, DB>(rows, b, d), q[d], s[b]);
     }
     const float factor = CAP || SLOPES ? 1.0f : c.factor;
+    const int limit = seen - key0 - 4 * half;      /* of the tile's keys, counted from this half's first, those below it are seen */
     const float away = (float)(place - key0 - 4 * half);
 #pragma unroll
     for (int b = 0; b < KB; ++b)
@@ -311,7 +312,7 @@ __device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVe
             if (CAP) v = __builtin_fmaf(-2.0f * c.high, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v * c.turn) + 1.0f), c.high);
             else if (SLOPES) v *= c.factor;
             if (SLOPES) v = __builtin_fmaf(-c.slope, __builtin_fabsf(away - (float)(32 * b + acc_row(r, 0))), v);
-            if (MASKED && key0 + 32 * b + acc_row(r, half) >= seen) v = -kInf;
+            if (MASKED && 32 * b + acc_row(r, 0) >= limit) v = -kInf;
             s[b][r] = v;
         }
     float most = s[0][0];
@@ -508,6 +509,7 @@ __device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, co
                                             int key0, int seen, int place, float lse2, const Score& c, int lane) {
     const int half = lane >> 5;
     const float away = (float)(place - key0 - 4 * half);
+    const int limit = seen - key0 - 4 * half;
     const uint32_t k_rows = reader.row + k_tile, v_rows = reader.row + v_tile;
     const ColumnPlace columns = reader.column + k_tile;
 #pragma unroll
@@ -523,7 +525,7 @@ __device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, co
         for (int r = 0; r < 16; ++r) {
             float steep;
             const float w = weight_of<CAP, SLOPES>(c, x[r], away - (float)(32 * b + acc_row(r, 0)), lse2, steep);
-            const bool hidden = MASKED && key0 + 32 * b + acc_row(r, half) >= seen;
+            const bool hidden = MASKED && 32 * b + acc_row(r, 0) >= limit;
             if (DELTA) delta += hidden ? 0.0f : w * dp[r];
             else x[r] = hidden ? 0.0f : (CAP ? w * steep : w) * (dp[r] - delta);
         }
@@ -641,12 +643,12 @@ struct Values {
     }
 };
 
-/* One tile of queries against the 32 keys of a wave.  stats: lse and delta of the tile's queries. */
+/* One tile of queries against the 32 keys of a wave.  stats: lse and delta of this half's queries; these see
+ * the lane's key (MASKED) from hidden_below on; away: from the key to the first of them. */
 template <typename T, int DB, bool CAP, bool SLOPES, bool MASKED, typename V>
 __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB], const typename HalfVec<T, 8>::type (&k)[2 * DB],
                                              const V& v, const Reader<DB>& reader, uint32_t q_tile, uint32_t g_tile,
-                                             const float* stats, const Shape& s, const Place& p, int prefix, int row0, int key, const Score& c, int lane) {
-    const int half = lane >> 5;
+                                             const float* stats, int hidden_below, float away, const Score& c, int lane) {
     f32x16 x = {}, dp = {};
 #pragma unroll
     for (int d = 0; d < 2 * DB; ++d) {
@@ -654,16 +656,15 @@ __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB],
         dp = mfma(read_row<T, DB>(reader.row + g_tile, 0, d), v[d], dp);
     }
     if (DB >= 3) __builtin_amdgcn_sched_barrier(0);    /* (nothing early: registers are short) */
-    const float away = (float)(row0 + p.m - p.n - key + 4 * half);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const float2 stat = *(const float2*)(stats + 2 * acc_row(r, half));
+        const float2 stat = *(const float2*)(stats + 2 * acc_row(r, 0));
         float steep;
-        float w = weight_of<CAP, SLOPES>(c, x[r], away + (float)acc_row(r, 0), stat.x, steep);
-        if (MASKED && key >= seen_by(s, p, prefix, row0 + acc_row(r, half))) w = 0.0f;
+        const float w = weight_of<CAP, SLOPES>(c, x[r], away + (float)acc_row(r, 0), stat.x, steep);
         const float ds = (CAP ? w * steep : w) * (dp[r] - stat.y);
-        dp[r] = MASKED && w == 0.0f ? 0.0f : ds;
-        x[r] = w;
+        const bool hidden = MASKED && acc_row(r, 0) < hidden_below;
+        x[r] = hidden ? 0.0f : w;
+        dp[r] = hidden ? 0.0f : ds;
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -724,6 +725,8 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
     int begin = 0;
     if (s.mask != L3_MASK_DOCUMENT && tile0 >= prefix) begin = min(max(tile0 - (p.m - p.n), 0), p.n) / kBackQueries * kBackQueries;
     const int steps = (p.n - begin + kBackQueries - 1) / kBackQueries, last = min(tile0 + kBackKeys, p.m);
+    const int from_key = key - (p.m - p.n) - 4 * half;                             /* of this half's queries, the one at the key's position */
+    const int sees_from = key < prefix ? -kBackQueries : from_key;                 /* ... the first that sees it */
     int masked = 0;
     while (masked < steps && seen_by(s, p, prefix, begin + masked * kBackQueries) < last) ++masked;
     const auto fetch = [&](int h, int i, int buffer) {
@@ -751,15 +754,15 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
             fetched();
             __syncthreads();
             fetch(h, i + 1, buffer ^ 1);
-            kv_grad_tile<T, DB, CAP, SLOPES, true>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), stats[buffer], s, p, prefix,
-                                                   begin + i * kBackQueries, key, score, lane);
+            kv_grad_tile<T, DB, CAP, SLOPES, true>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), &stats[buffer][8 * half], sees_from - begin - i * kBackQueries,
+                                                   (float)(begin + i * kBackQueries - from_key), score, lane);
         }
         for (; i < steps; ++i, buffer ^= 1) {
             fetched();
             __syncthreads();
             fetch(h, i + 1, buffer ^ 1);
-            kv_grad_tile<T, DB, CAP, SLOPES, false>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), stats[buffer], s, p, prefix,
-                                                    begin + i * kBackQueries, key, score, lane);
+            kv_grad_tile<T, DB, CAP, SLOPES, false>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), &stats[buffer][8 * half], 0,
+                                                    (float)(begin + i * kBackQueries - from_key), score, lane);
         }
     }
     if (key >= p.m) return;
@@ -1037,7 +1040,7 @@ l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
 int splits_of(const Shape& s) {
     const int64_t tiles = most_tiles(s.kv_tokens, s.images, kBackKeys) * s.kv_heads;
     int splits = 1;
-    while (splits < s.group && (tiles * splits < 1024 || s.group % splits)) ++splits;
+    while (splits < s.group && (tiles * splits < (s.mask == L3_MASK_DOCUMENT ? 1024 : 2048) || s.group % splits)) ++splits;
     return splits;
 }
 
