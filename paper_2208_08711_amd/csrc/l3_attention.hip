@@ -353,6 +353,81 @@ __device__ __forceinline__ void one_tile(Running<DB>& run, const typename HalfVe
         }
 }
 
+/* Keys begin .. end - 1 in tiles of 32 that the waves of a workgroup take in turn, each on its own, with two
+ * stages of keys and values in `own` local memory.  Tiles below `whole` need no mask. */
+template <typename T, int DB, bool CAP, bool SLOPES, int WAVES>
+__device__ __forceinline__ void run_wave(Running<DB>& run, const typename HalfVec<T, 8>::type (&q)[2 * DB], uint32_t own, const T* k, int64_t k_stride,
+                                         const T* v, int64_t v_stride, int dim, int begin, int end, int whole, int seen, int place, const Score& score,
+                                         int lane, int wave) {
+    constexpr int kTile = 32 * Tile<DB>::kPitch;
+    const Reader<DB> reader(lane);
+    Fetch<DB, 32, 64> fetch_k, fetch_v;
+    fetch_k.set(k_stride, dim, lane);
+    fetch_v.set(v_stride, dim, lane);
+    const auto fetch = [&](int key0, int stage) {
+        if (key0 >= end) return;
+        fetch_k(own + stage * 2 * kTile, k + key0 * k_stride, end - key0, lane);
+        fetch_v(own + stage * 2 * kTile + kTile, v + key0 * v_stride, end - key0, lane);
+    };
+    int stage = 0, key0 = begin + wave * 32;
+    fetch(key0, 0);
+    for (; key0 + 32 <= whole; key0 += WAVES * 32, stage ^= 1) {
+        fetched();
+        fetch(key0 + WAVES * 32, stage ^ 1);
+        one_tile<T, DB, 32, CAP, SLOPES, false>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, seen, place, score, lane);
+        /* this wave's reads of the tile have come back before the next fetch into it is sent */
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    for (; key0 < end; key0 += WAVES * 32, stage ^= 1) {
+        fetched();
+        fetch(key0 + WAVES * 32, stage ^ 1);
+        one_tile<T, DB, 32, CAP, SLOPES, true>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, seen, place, score, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+/* Local memory of a workgroup of WAVES such waves, which what they join takes over */
+template <int DB, int WAVES>
+constexpr int wave_room() {
+    constexpr int tiles = WAVES * 4 * 32 * Tile<DB>::kPitch, join = WAVES * (2 * 32 + 32 * DB * 32) * 4;
+    return tiles > join ? tiles : join;
+}
+
+/* The waves' reference points, sums and products joined: store(query, element, product, top, sum) for
+ * each of 32 queries and dim elements, the last two the same for all elements of a query. */
+template <int DB, int WAVES, typename STORE>
+__device__ __forceinline__ void join_waves(const Running<DB>& run, uint8_t* room, int dim, int lane, int wave, STORE store) {
+    __syncthreads();
+    float* const tops = (float*)room;                              /* [waves][32], then sums, then products */
+    float* const sums = tops + WAVES * 32;
+    float* const products = sums + WAVES * 32;                     /* [waves][32 * DB][32] */
+    const float sum = across_sum(run.sum);
+    if (lane < 32) {
+        tops[wave * 32 + lane] = run.top;
+        sums[wave * 32 + lane] = sum;
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) products[(wave * 32 * DB + 32 * d + acc_row(r, lane >> 5)) * 32 + (lane & 31)] = run.out[d][r];
+    __syncthreads();
+    const int g = threadIdx.x & 31;
+    float top = -kInf, total = 0.0f, f[WAVES];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w * 32 + g]);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        f[w] = tops[w * 32 + g] > -kInf ? __builtin_amdgcn_exp2f(tops[w * 32 + g] - top) : 0.0f;
+        total = __builtin_fmaf(f[w], sums[w * 32 + g], total);
+    }
+    for (int c = threadIdx.x / 32; c < dim; c += WAVES * 2) {
+        float x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x = __builtin_fmaf(f[w], products[(w * 32 * DB + c) * 32 + g], x);
+        store(g, c, x, top, total);
+    }
+}
+
 struct Heads {
     const void* d;
     int64_t token, head;
@@ -444,6 +519,37 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kernel(ForwardArgs a
             store_narrow<T, 4>(out + c, x);
         }
     if (a.lse && half == 0) a.lse[(int64_t)head * s.q_tokens + p.q0 + row] = seen > 0 ? (run.top + __builtin_amdgcn_logf(sum)) * kLn2 : -kInf;
+}
+
+/* The same with 32 queries a workgroup, whose waves share the keys: where workgroups of 128 queries would
+ * leave CUs idle, four times as many of a quarter of the length. */
+template <typename T, int DB, bool CAP, bool SLOPES>
+__global__ __launch_bounds__(kThreads, 1) void l3_attention_few_kernel(ForwardArgs a) {
+    __shared__ __attribute__((aligned(256))) uint8_t room[wave_room<DB, 4>()];
+    const Shape& s = a.s;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
+    const Place p = find_tile(s, index, 32, false);
+    if (p.image < 0) return;
+    const int prefix = prefix_of(s, p);
+    const int row0 = p.tile * 32, row = row0 + (lane & 31);
+    const int all = seen_by(s, p, prefix, min(row0 + 31, p.n - 1)), whole = seen_by(s, p, prefix, row0);
+    const int seen = row < p.n ? seen_by(s, p, prefix, row) : 0;
+    const Score score = score_of(s.scale, s.cap, SLOPES ? s.slopes[head] : 0.0f);
+    typename HalfVec<T, 8>::type q[2 * DB];
+    load_operand<T, DB>(q, (const T*)a.q.d + (int64_t)(p.q0 + row) * a.q.token + (int64_t)head * a.q.head, row < p.n, s.head_dim, half);
+    Running<DB> run;
+    run.start();
+    run_wave<T, DB, CAP, SLOPES, 4>(run, q, lds_address(room) + wave * 4 * 32 * Tile<DB>::kPitch,
+                                    (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head, a.k.token,
+                                    (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head, a.v.token, s.head_dim, 0, all, whole, seen,
+                                    row + p.m - p.n, score, lane, wave);
+    join_waves<DB, 4>(run, room, s.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
+        if (row0 + g >= p.n) return;
+        const bool any = seen_by(s, p, prefix, row0 + g) > 0;
+        ((T*)const_cast<void*>(a.out.d))[(int64_t)(p.q0 + row0 + g) * a.out.token + (int64_t)head * a.out.head + c] = (T)(any ? x / total : 0.0f);
+        if (c == 0 && a.lse) a.lse[(int64_t)head * s.q_tokens + p.q0 + row0 + g] = any ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -kInf;
+    });
 }
 
 /* ---- gradients ----------------------------------------------------------------------------- */
@@ -842,7 +948,7 @@ struct StepArgs {
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(StepArgs a) {
     constexpr int kTile = kStepKeys * Tile<DB>::kPitch;
-    extern __shared__ __attribute__((aligned(256))) uint8_t step_lds[];
+    __shared__ __attribute__((aligned(256))) uint8_t room[wave_room<DB, kStepWaves>()];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     /* heads side by side in memory are read side by side in time */
     int at = blockIdx.x;
@@ -862,63 +968,17 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
     const Score score = score_of(a.scale, a.cap, SLOPES && there ? a.slopes[head] : 0.0f);
     const T* const k = (const T*)a.k.d + (int64_t)sequence * a.k_sequence + (int64_t)kv_head * a.k.head;
     const T* const v = (const T*)a.v.d + (int64_t)sequence * a.v_sequence + (int64_t)kv_head * a.v.head;
-    const uint32_t own = lds_address(step_lds) + wave * 4 * kTile;              /* 2 stages of keys and values */
     const Reader<DB> reader(lane);
     Running<DB> run;
     run.start();
-    const int first = begin + wave * kStepKeys;
-    Fetch<DB, kStepKeys, 64> fetch_k, fetch_v;
-    fetch_k.set(a.k.token, a.head_dim, lane);
-    fetch_v.set(a.v.token, a.head_dim, lane);
-    const auto fetch = [&](int key0, int stage) {
-        if (key0 >= end) return;
-        fetch_k(own + stage * 2 * kTile, k + key0 * a.k.token, end - key0, lane);
-        fetch_v(own + stage * 2 * kTile + kTile, v + key0 * a.v.token, end - key0, lane);
-    };
-    fetch(first, 0);
-    int stage = 0, key0 = first;
-    for (; key0 + kStepKeys <= end; key0 += kStepWaves * kStepKeys, stage ^= 1) {
-        fetched();
-        fetch(key0 + kStepWaves * kStepKeys, stage ^ 1);
-        one_tile<T, DB, kStepKeys, CAP, SLOPES, false>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, length - 1, score, lane);
-        /* this wave's reads of the tile have come back before the next fetch into it is sent */
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    if (key0 < end) {
-        fetched();
-        one_tile<T, DB, kStepKeys, CAP, SLOPES, true>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, end, length - 1, score, lane);
-    }
-
-    /* join the waves: reference point, sum and products of each through local memory */
-    __syncthreads();
-    float* const tops = (float*)step_lds;                          /* [waves][32], then sums, then products */
-    float* const sums = tops + kStepWaves * 32;
-    float* const products = sums + kStepWaves * 32;                         /* [waves][32 * DB][32] */
-    const float sum = across_sum(run.sum);
-    if (half == 0) {
-        tops[wave * 32 + lane] = run.top;
-        sums[wave * 32 + lane] = sum;
-    }
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) products[(wave * 32 * DB + 32 * d + acc_row(r, half)) * 32 + (lane & 31)] = run.out[d][r];
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * a.head_dim; i += kStepThreads) {
-        const int g = i / a.head_dim, c = i - g * a.head_dim;
-        if (of * 32 + g >= a.group) break;
-        float top = -kInf;
-        for (int w = 0; w < kStepWaves; ++w) top = fmaxf(top, tops[w * 32 + g]);
-        float total = 0.0f, x = 0.0f;
-        for (int w = 0; w < kStepWaves; ++w) {
-            const float f = tops[w * 32 + g] > -kInf ? __builtin_amdgcn_exp2f(tops[w * 32 + g] - top) : 0.0f;
-            total += f * sums[w * 32 + g];
-            x += f * products[(w * 32 * DB + c) * 32 + g];
-        }
+    run_wave<T, DB, CAP, SLOPES, kStepWaves>(run, q, lds_address(room) + wave * 4 * kTile, k, a.k.token, v, a.v.token, a.head_dim, begin, end, end, end,
+                                             length - 1, score, lane, wave);
+    join_waves<DB, kStepWaves>(run, room, a.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
+        if (of * 32 + g >= a.group) return;
         const int64_t h = kv_head * a.group + of * 32 + g;
         if (!a.partial) {
             ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + h * a.out.head + c] = (T)(length > 0 ? x / total : 0.0f);
-            continue;
+            return;
         }
         float* const record = a.partial + (((int64_t)sequence * a.q_heads + h) * a.chunks + chunk) * (a.head_dim + kStepRecord);
         record[kStepRecord + c] = x;
@@ -926,7 +986,7 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
             record[0] = top;
             record[1] = total;
         }
-    }
+    });
 }
 
 /* The chunks of a sequence and head joined; one workgroup a head, one thread an element. */
@@ -1023,13 +1083,23 @@ void by_score(bool cap, bool slopes, F f) {
     else f(std::false_type(), std::false_type());
 }
 
+/* Does a forward call leave CUs idle, with enough keys to share?  Measured (64 wide, one image unless said; workgroups of
+ * 128 queries against 32): 4 heads x 1000 tokens (32 workgroups of 128) 18.2 and 11.5 us, 12 x 1000 causal (96) 18.3 and 13.3,
+ * 4 x 4000 128 wide (128) 83 and 72, 12 x 2000 (192) 33.8 and 36.7; 6 heads x 200 tokens 7.7 and 6.8, x 64 4.6 and 5.9. */
+bool few_queries(const Shape& s, int64_t workgroups) { return workgroups <= 128 && s.kv_tokens >= 192 * (int64_t)s.images; }
+
 template <typename T>
 l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
-    const int64_t grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
+    int64_t grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
     if (grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    const bool few = few_queries(a.s, grid);
+    if (few) grid = most_tiles(a.s.q_tokens, a.s.images, 32) * a.s.q_heads;
     by_width(a.s.head_dim, [&](auto db) {
         by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
-            hipLaunchKernelGGL((l3_attention_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+            if (few)
+                hipLaunchKernelGGL((l3_attention_few_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+            else
+                hipLaunchKernelGGL((l3_attention_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
         });
     });
     return launched();
@@ -1086,10 +1156,8 @@ l3_status run_step(const StepArgs& a, hipStream_t stream) {
     if (grid >= (int64_t)1 << 31 || (int64_t)a.n * a.q_heads >= (int64_t)1 << 31) return L3_ERR_LIMIT;
     by_width(a.head_dim, [&](auto db) {
         by_score(a.cap > 0.0f, a.slopes != nullptr, [&](auto cap, auto slopes) {
-            const size_t tiles = kStepWaves * 4 * (size_t)kStepKeys * Tile<db.value>::kPitch;
-            const size_t join = kStepWaves * (2 * 32 + 32 * db.value * 32) * sizeof(float);
-            hipLaunchKernelGGL((l3_attention_step_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kStepThreads),
-                               std::max(tiles, join), stream, a);
+            hipLaunchKernelGGL((l3_attention_step_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kStepThreads), 0,
+                               stream, a);
         });
     });
     if (launched() != L3_OK) return L3_ERR_DEVICE;
