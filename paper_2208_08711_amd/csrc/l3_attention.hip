@@ -559,8 +559,11 @@ struct BackwardArgs {
     Heads q, k, v, out, out_grad, q_grad, k_grad, v_grad;
     const float* lse;
     float* stats;                          /* [q_heads][q_tokens][2]: lse in log2 and delta = dot(out, its gradient) */
-    float* partial;                        /* [2][splits][kv_tokens][kv_heads][head_dim], where splits > 1 */
-    int32_t splits;                        /* workgroups that share a tile of keys, each with some of the query heads */
+    float* partial;                        /* 32-bit gradients of each split, where there is more than one: [splits][tokens][heads][head_dim],
+                                              of the queries, then (in its place) of the keys and behind them of the values */
+    int32_t q_splits;                      /* workgroups that share a tile of queries, each with some of the keys */
+    int32_t head_splits, row_splits;       /* their product: workgroups that share a tile of keys, each with some of the query heads
+                                              and of their queries */
 };
 
 /* lse to log2 (+inf, so that all weights are 0, for a query that sees nothing); delta: 16 lanes a
@@ -658,7 +661,10 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
     const auto tile = [&](int buffer, int which) { return tiles_at + (2 * buffer + which) * (uint32_t)(kKeys * Tile<DB>::kPitch); };
     const Shape& s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int index = blockIdx.x / s.q_heads, head = blockIdx.x - index * s.q_heads, kv_head = head / s.group;
+    int at = blockIdx.x;
+    const int split = at % a.q_splits;
+    at /= a.q_splits;
+    const int index = at / s.q_heads, head = at - index * s.q_heads, kv_head = head / s.group;
     Place p = find_tile(s, index, kQueries, false);
     if (p.image < 0) return;
     p.tile = (p.n + kQueries - 1) / kQueries - 1 - p.tile;
@@ -687,32 +693,34 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
 #pragma unroll
     for (int d = 0; d < DB; ++d) grad[d] = f32x16{};
     const int steps = (all + kKeys - 1) / kKeys, plain = whole / kKeys;
+    const int begin = steps <= kExactSteps ? (split ? steps : 0) : (int)((int64_t)steps * split / a.q_splits);
+    const int end = steps <= kExactSteps ? steps : (int)((int64_t)steps * (split + 1) / a.q_splits);
     const auto fetch = [&](int i) {
-        if (i >= steps) return;
+        if (i >= end) return;
         fetch_k(tile(i & 1, 0), k + (int64_t)i * kKeys * a.k.token, p.m - i * kKeys, threadIdx.x);
         fetch_v(tile(i & 1, 1), v + (int64_t)i * kKeys * a.v.token, p.m - i * kKeys, threadIdx.x);
     };
-    fetch(0);
+    fetch(begin);
     if (steps <= kExactSteps) {
-        fetch(1);
+        fetch(begin + 1);
         fetched();
         __syncthreads();
         float sum = 0.0f;
-        for (int i = 0; i < steps; ++i)
+        for (int i = begin; i < end; ++i)
             q_grad_tile<T, DB, CAP, SLOPES, true, true>(grad, sum, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
         delta = across_sum(sum);
-        if (row < p.n && half == 0) stats[1] = delta;
-        for (int i = 0; i < steps; ++i)
+        if (row < p.n && half == 0 && split == 0) stats[1] = delta;
+        for (int i = begin; i < end; ++i)
             q_grad_tile<T, DB, CAP, SLOPES, true, false>(grad, delta, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
     } else {
-        int i = 0;
-        for (; i < plain; ++i) {
+        int i = begin;
+        for (; i < min(plain, end); ++i) {
             fetched();
             __syncthreads();
             fetch(i + 1);
             q_grad_tile<T, DB, CAP, SLOPES, false, false>(grad, delta, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
         }
-        for (; i < steps; ++i) {
+        for (; i < end; ++i) {
             fetched();
             __syncthreads();
             fetch(i + 1);
@@ -720,6 +728,7 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
         }
     }
     if (row >= p.n) return;
+    float* const part = a.partial + (((int64_t)split * s.q_tokens + p.q0 + row) * s.q_heads + head) * s.head_dim;
     T* const out = (T*)const_cast<void*>(a.q_grad.d) + (int64_t)(p.q0 + row) * a.q_grad.token + (int64_t)head * a.q_grad.head;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -730,7 +739,8 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
             float y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = grad[d][4 * e + i] * s.scale;
-            store_narrow<T, 4>(out + c, y);
+            if (a.q_splits > 1) *(float4*)(part + c) = float4{y[0], y[1], y[2], y[3]};
+            else store_narrow<T, 4>(out + c, y);
         }
 }
 
@@ -798,15 +808,15 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
     const Shape& s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     int at = blockIdx.x;
-    const int split = at % a.splits;
-    at /= a.splits;
+    const int splits = a.head_splits * a.row_splits, split = at % splits, head_split = split / a.row_splits, row_split = split - head_split * a.row_splits;
+    at /= splits;
     const int index = at / s.kv_heads, kv_head = at - index * s.kv_heads;
     const Place p = find_tile(s, index, kBackKeys, true);
     if (p.image < 0) return;
     const int prefix = prefix_of(s, p);
     const int tile0 = p.tile * kBackKeys;
     const int key = tile0 + wave * 32 + (lane & 31);
-    const int heads = s.group / a.splits, head0 = kv_head * s.group + split * heads;
+    const int heads = s.group / a.head_splits, head0 = kv_head * s.group + head_split * heads;
 
     const Reader<DB> reader(lane);
     typename HalfVec<T, 8>::type k[2 * DB];
@@ -830,17 +840,18 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
     /* queries from `begin` on see keys of the workgroup; from the tile at `plain` on they see all of them */
     int begin = 0;
     if (s.mask != L3_MASK_DOCUMENT && tile0 >= prefix) begin = min(max(tile0 - (p.m - p.n), 0), p.n) / kBackQueries * kBackQueries;
-    const int steps = (p.n - begin + kBackQueries - 1) / kBackQueries, last = min(tile0 + kBackKeys, p.m);
+    const int all = (p.n - begin + kBackQueries - 1) / kBackQueries, last = min(tile0 + kBackKeys, p.m);
+    const int from = (int)((int64_t)all * row_split / a.row_splits), to = (int)((int64_t)all * (row_split + 1) / a.row_splits);   /* this split's tiles */
     const int from_key = key - (p.m - p.n) - 4 * half;                             /* of this half's queries, the one at the key's position */
     const int sees_from = key < prefix ? -kBackQueries : from_key;                 /* ... the first that sees it */
-    int masked = 0;
-    while (masked < steps && seen_by(s, p, prefix, begin + masked * kBackQueries) < last) ++masked;
+    int masked = from;
+    while (masked < to && seen_by(s, p, prefix, begin + masked * kBackQueries) < last) ++masked;
     const auto fetch = [&](int h, int i, int buffer) {
-        if (i >= steps) {
-            i = 0;
+        if (i >= to) {
+            i = from;
             ++h;
         }
-        if (h >= heads || steps == 0) return;
+        if (h >= heads || from == to) return;
         const int row0 = begin + i * kBackQueries;
         const int64_t row = (int64_t)p.q0 + row0;
         fetch_q(tile(buffer, 0), (const T*)a.q.d + row * a.q.token + (int64_t)(head0 + h) * a.q.head, p.n - row0, threadIdx.x);
@@ -851,11 +862,11 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
                              min(p.n - row0, kBackQueries) * 8, threadIdx.x * 4);
         }
     };
-    fetch(0, 0, 0);
+    fetch(0, from, 0);
     int buffer = 0;
     for (int h = 0; h < heads; ++h) {
         const Score score = score_of(s.scale, s.cap, SLOPES ? s.slopes[head0 + h] : 0.0f);
-        int i = 0;
+        int i = from;
         for (; i < masked; ++i, buffer ^= 1) {
             fetched();
             __syncthreads();
@@ -863,7 +874,7 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
             kv_grad_tile<T, DB, CAP, SLOPES, true>(dk, dv, k, v, reader, tile(buffer, 0), tile(buffer, 1), &stats[buffer][8 * half], sees_from - begin - i * kBackQueries,
                                                    (float)(begin + i * kBackQueries - from_key), score, lane);
         }
-        for (; i < steps; ++i, buffer ^= 1) {
+        for (; i < to; ++i, buffer ^= 1) {
             fetched();
             __syncthreads();
             fetch(h, i + 1, buffer ^ 1);
@@ -875,7 +886,7 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
     const int64_t row = p.k0 + key;
     T* const k_out = (T*)const_cast<void*>(a.k_grad.d) + row * a.k_grad.token + (int64_t)kv_head * a.k_grad.head;
     T* const v_out = (T*)const_cast<void*>(a.v_grad.d) + row * a.v_grad.token + (int64_t)kv_head * a.v_grad.head;
-    const int64_t plane = (int64_t)a.splits * s.kv_tokens * s.kv_heads * s.head_dim;
+    const int64_t plane = (int64_t)splits * s.kv_tokens * s.kv_heads * s.head_dim;
     float* const part = a.partial + (((int64_t)split * s.kv_tokens + row) * s.kv_heads + kv_head) * s.head_dim;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -889,7 +900,7 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
                 y[i] = dk[d][4 * e + i] * s.scale;
                 z[i] = dv[d][4 * e + i];
             }
-            if (a.splits > 1) {
+            if (splits > 1) {
                 *(float4*)(part + c) = float4{y[0], y[1], y[2], y[3]};
                 *(float4*)(part + plane + c) = float4{z[0], z[1], z[2], z[3]};
             } else {
@@ -899,29 +910,29 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
         }
 }
 
-/* The splits' sums joined, in order; 4 elements a thread, of keys and values. */
+/* The splits' sums joined, in order: 4 elements a thread, of all tokens below the table's end. */
 template <typename T>
-__global__ __launch_bounds__(kThreads) void l3_attention_kv_join_kernel(BackwardArgs a) {
-    const Shape& s = a.s;
-    const int64_t plane = (int64_t)s.kv_tokens * s.kv_heads * s.head_dim;
+__global__ __launch_bounds__(kThreads) void l3_attention_grad_join_kernel(const float* partial, int splits, const int32_t* first, int images, int tokens, int heads,
+                                                                          int head_dim, Heads to, Heads to_second) {
+    const int64_t plane = (int64_t)tokens * heads * head_dim;
     const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
     if (at >= plane) return;
-    const int64_t row = at / (s.kv_heads * s.head_dim);
-    if (row >= first_of(s.kv_first, s.images, s.kv_tokens)) return;
-    const int rest = (int)(at - row * (s.kv_heads * s.head_dim)), head = rest / s.head_dim, c = rest - head * s.head_dim;
-#pragma unroll
+    const int64_t row = at / (heads * head_dim);
+    if (row >= first_of(first, images, tokens)) return;
+    const int rest = (int)(at - row * (heads * head_dim)), head = rest / head_dim, c = rest - head * head_dim;
     for (int which = 0; which < 2; ++which) {
-        const float* from = a.partial + which * a.splits * plane + at;
+        const Heads& out = which ? to_second : to;
+        if (!out.d) break;
+        const float* from = partial + which * splits * plane + at;
         float x[4] = {};
-        for (int i = 0; i < a.splits; ++i, from += plane) {
+        for (int i = 0; i < splits; ++i, from += plane) {
             const float4 v = *(const float4*)from;
             x[0] += v.x;
             x[1] += v.y;
             x[2] += v.z;
             x[3] += v.w;
         }
-        const Heads& to = which ? a.v_grad : a.k_grad;
-        store_narrow<T, 4>((T*)const_cast<void*>(to.d) + row * to.token + (int64_t)head * to.head + c, x);
+        store_narrow<T, 4>((T*)const_cast<void*>(out.d) + row * out.token + (int64_t)head * out.head + c, x);
     }
 }
 
@@ -1105,39 +1116,76 @@ l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
     return launched();
 }
 
-/* Workgroups that share a tile of keys: as few (of the divisors of the heads that share it) as give every CU
- * four.  Each more is a 32-bit copy of the gradients to write and to add up. */
-int splits_of(const Shape& s) {
+/* How the gradients are split.  Workgroups that share a tile of keys: of the query heads that share it as few
+ * parts (divisors of their number) as give every CU four, twice that under masks, whose tiles differ in work; and where
+ * that leaves CUs idle, parts of the queries of 256 or more.  Workgroups that share a tile of queries: parts of the keys
+ * likewise.  Each part is a 32-bit copy of the gradients to write and to add up. */
+struct Splits {
+    int q, head, row;
+    int kv() const { return head * row; }
+};
+
+/* (Forward and gradients, 64 wide: 4 heads x 1000 tokens 67 us in one part, 53 in parts; 12 x 2000 136 and 128;
+ * 4 heads on 1 x 4000 causal, 128 wide, 393 and 197; but 4 images x 12 x 1000, 384 workgroups of queries, 108 and 120,
+ * 8 x 8000, 504, 651 and 699.  Masks leave tiles of little work: twice as many.) */
+int parts_of(const Shape& s, int64_t workgroups, int64_t length) {
+    const int64_t enough = s.mask == L3_MASK_DOCUMENT ? 256 : 512;
+    int parts = 1;
+    while (parts < 8 && workgroups * parts < enough && length >= 512 * (int64_t)parts) parts *= 2;
+    return parts;
+}
+
+Splits splits_of(const Shape& s) {
+    Splits splits = {1, 1, 1};
+    if (!s.images) return splits;
     const int64_t tiles = most_tiles(s.kv_tokens, s.images, kBackKeys) * s.kv_heads;
-    int splits = 1;
-    while (splits < s.group && (tiles * splits < (s.mask == L3_MASK_DOCUMENT ? 1024 : 2048) || s.group % splits)) ++splits;
+    while (splits.head < s.group && (tiles * splits.head < (s.mask == L3_MASK_DOCUMENT ? 1024 : 2048) || s.group % splits.head)) ++splits.head;
+    splits.row = parts_of(s, tiles * splits.head, s.q_tokens / s.images);
+    splits.q = parts_of(s, most_tiles(s.q_tokens, s.images, kQueries) * s.q_heads, s.kv_tokens / s.images);
     return splits;
 }
 
 size_t stats_bytes(const Shape& s) { return ((size_t)s.q_heads * (size_t)s.q_tokens * 2 * sizeof(float) + 15) / 16 * 16; }
 
+size_t partial_bytes(const Shape& s) {
+    const Splits splits = splits_of(s);
+    const size_t of_q = splits.q > 1 ? (size_t)splits.q * s.q_tokens * s.q_heads : 0;
+    const size_t of_kv = splits.kv() > 1 ? 2 * (size_t)splits.kv() * s.kv_tokens * s.kv_heads : 0;
+    return std::max(of_q, of_kv) * s.head_dim * sizeof(float);
+}
+
 template <typename T>
 l3_status run_backward(const BackwardArgs& a, hipStream_t stream) {
-    const int64_t q_grid = most_tiles(a.s.q_tokens, a.s.images, kQueries) * a.s.q_heads;
-    const int64_t kv_grid = most_tiles(a.s.kv_tokens, a.s.images, kBackKeys) * a.s.kv_heads * a.splits;
-    const int64_t stats_grid = ((int64_t)a.s.q_tokens * a.s.q_heads * 16 + kThreads - 1) / kThreads;
-    const int64_t join_grid = a.splits > 1 ? ((int64_t)a.s.kv_tokens * a.s.kv_heads * a.s.head_dim / 4 + kThreads - 1) / kThreads : 0;
-    if (q_grid >= (int64_t)1 << 31 || kv_grid >= (int64_t)1 << 31 || stats_grid >= (int64_t)1 << 31 || join_grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    const Shape& s = a.s;
+    const int splits = a.head_splits * a.row_splits;
+    const auto blocks = [](int64_t threads) { return (threads + kThreads - 1) / kThreads; };
+    const int64_t q_grid = most_tiles(s.q_tokens, s.images, kQueries) * s.q_heads * a.q_splits;
+    const int64_t kv_grid = most_tiles(s.kv_tokens, s.images, kBackKeys) * s.kv_heads * splits;
+    const int64_t stats_grid = blocks((int64_t)s.q_tokens * s.q_heads * 16);
+    const int64_t q_join = a.q_splits > 1 ? blocks((int64_t)s.q_tokens * s.q_heads * s.head_dim / 4) : 0;
+    const int64_t kv_join = splits > 1 ? blocks((int64_t)s.kv_tokens * s.kv_heads * s.head_dim / 4) : 0;
+    for (const int64_t grid : {q_grid, kv_grid, stats_grid, q_join, kv_join})
+        if (grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
     if (stats_grid) hipLaunchKernelGGL((l3_attention_stats_kernel<T>), dim3((unsigned)stats_grid), dim3(kThreads), 0, stream, a);
     if (launched() != L3_OK) return L3_ERR_DEVICE;
-    by_width(a.s.head_dim, [&](auto db) {
-        by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
+    by_width(s.head_dim, [&](auto db) {
+        by_score(s.cap > 0.0f, s.slopes != nullptr, [&](auto cap, auto slopes) {
             /* (queries first: they leave better deltas) */
             if (q_grid)
                 hipLaunchKernelGGL((l3_attention_q_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)q_grid), dim3(kThreads), 0,
                                    stream, a);
+            if (q_join)
+                hipLaunchKernelGGL((l3_attention_grad_join_kernel<T>), dim3((unsigned)q_join), dim3(kThreads), 0, stream, a.partial, a.q_splits,
+                                   s.q_first, s.images, s.q_tokens, s.q_heads, s.head_dim, a.q_grad, Heads{});
             if (kv_grid)
                 hipLaunchKernelGGL((l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)kv_grid), dim3(kThreads), 0,
                                    stream, a);
         });
     });
     if (launched() != L3_OK) return L3_ERR_DEVICE;
-    if (join_grid) hipLaunchKernelGGL((l3_attention_kv_join_kernel<T>), dim3((unsigned)join_grid), dim3(kThreads), 0, stream, a);
+    if (kv_join)
+        hipLaunchKernelGGL((l3_attention_grad_join_kernel<T>), dim3((unsigned)kv_join), dim3(kThreads), 0, stream, a.partial, splits, s.kv_first, s.images,
+                           s.kv_tokens, s.kv_heads, s.head_dim, a.k_grad, a.v_grad);
     return launched();
 }
 
@@ -1188,8 +1236,7 @@ size_t l3_attention_workspace(const l3_attention_shape* shape) {
     bool nothing = false;
     if (check_shape(shape, &nothing) != L3_OK) return 0;
     const Shape s = shape_of(*shape);
-    const size_t splits = (size_t)splits_of(s);
-    return 16 + stats_bytes(s) + (splits > 1 ? 2 * splits * (size_t)s.kv_tokens * s.kv_heads * s.head_dim * sizeof(float) : 0);
+    return 16 + stats_bytes(s) + partial_bytes(s);
 }
 
 l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3_heads q, l3_heads k, l3_heads v,
@@ -1209,8 +1256,10 @@ l3_status l3_attention_backward(l3_ctx* ctx, const l3_attention_shape* shape, l3
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     const Shape s = shape_of(*shape);
+    const Splits splits = splits_of(s);
     const BackwardArgs a = {s, heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(out_grad), heads_of(q_grad),
-                            heads_of(k_grad), heads_of(v_grad), d_lse, (float*)d_workspace, (float*)((uint8_t*)d_workspace + stats_bytes(s)), splits_of(s)};
+                            heads_of(k_grad), heads_of(v_grad), d_lse, (float*)d_workspace, (float*)((uint8_t*)d_workspace + stats_bytes(s)), splits.q, splits.head,
+                            splits.row};
     return shape->dtype == L3_BF16 ? run_backward<__bf16>(a, (hipStream_t)stream) : run_backward<_Float16>(a, (hipStream_t)stream);
 }
 

@@ -388,6 +388,15 @@ def test_attention_lengths(l3, ctx, lengths):
     run_attention(l3, ctx, lengths, None, (1, 1), 128, torch.float16, 0, 0.0, False, behind=0)
 
 
+@pytest.mark.parametrize("mask", (0, 1, 2))
+@pytest.mark.parametrize("heads,head_dim,dtype", (((2, 2), 64, torch.bfloat16), ((4, 1), 128, torch.float16)))
+def test_attention_long_images_and_few_heads(l3, ctx, heads, head_dim, dtype, mask):
+    """Gradients whose keys and queries are shared out among workgroups, with images too short for that beside
+    long ones; forward calls whose waves share the keys."""
+    run_attention(l3, ctx, (1500, 3, 0, 700, 131), None, heads, head_dim, dtype, mask, 0.0, False)
+    run_attention(l3, ctx, (2100, 40), (1100, 1900), heads, head_dim, dtype, mask, 0.0, False)
+
+
 def test_attention_scores_far_apart(l3, ctx):
     """Scores that grow along the keys by far more than the reference point may lag, and large negative ones."""
     n, d = 300, 64
