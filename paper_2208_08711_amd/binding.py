@@ -490,18 +490,36 @@ def patch_tokens_count(width, height, side):
     return int(_load().l3_patch_tokens_count(int(width), int(height), int(side)))
 
 
+# patch_tokens_batch relies on this layout
+assert ctypes.sizeof(_TokenImage) == 24 and _TokenImage.width.offset == 16 and _TokenImage.height.offset == 20
+_stride, _get_device, _dtype = operator.methodcaller("stride"), operator.methodcaller("get_device"), operator.attrgetter("dtype")
+
+
 def patch_tokens_batch(ctx, images, side, mean, stdv, tokens, positions=None, first=None, stream=None, row_strides=None):
     """images: list of uint8 device tensors [H, W, 3] (pixels side by side; rows contiguous unless their
     strides say otherwise or row_strides is given); tokens: device tensor [total, 3*side*side]; positions: int32
     [total, 2] or None; first: int32 [len(images) + 1] or None.  Enqueues on `stream` (default: torch's current)."""
     n = len(images)
-    kind, index = _common([tokens], (positions, first, *images))
-    arr = (_TokenImage * max(n, 1))()
-    for i, image in enumerate(images):
-        if image.dtype is not _torch.uint8 or image.dim() != 3 or image.shape[2] != 3 or image.stride(2) != 1 or image.stride(1) != 3:
-            raise ValueError("expected uint8 [H, W, 3] with pixels side by side")
-        arr[i].d_rgb, arr[i].height, arr[i].width = image.data_ptr(), image.shape[0], image.shape[1]
-        arr[i].row_stride = max(image.stride(0), 3 * image.shape[1]) if row_strides is None else row_strides[i]
+    kind, index = _common([tokens], (positions, first))
+    if n and (set(map(_dtype, images)) != {_torch.uint8} or set(map(_get_device, images)) != {index}):
+        raise ValueError("expected uint8 images on the GPU of the tokens")
+    # the l3_token_image array, three words of 8 bytes each, filled column by column as in encode_batch
+    # (256 photographs: 330 us image by image, a third so)
+    words, sides, rows = array.array("Q", bytes(24 * n)), [], []
+    try:
+        for (h, w, c), (row, pixel, channel) in zip(map(_shape, images), map(_stride, images)):
+            if c != 3 or pixel != 3 or channel != 1:
+                raise ValueError
+            sides.append(w & _MASK32 | (h & _MASK32) << 32)
+            rows.append(row if row > 3 * w else 3 * w)
+    except ValueError:
+        raise ValueError("expected [H, W, 3] images with pixels side by side") from None
+    if row_strides is not None:
+        rows = [operator.index(row_strides[i]) & _MASK64 for i in range(n)]
+    words[0::3] = array.array("Q", map(_data_ptr, images))
+    words[1::3] = array.array("Q", rows)
+    words[2::3] = array.array("Q", sides)
+    arr = (_TokenImage * n).from_buffer(words) if n else (_TokenImage * 1)()
     if tokens.dim() != 2 or not tokens.is_contiguous() or tokens.shape[1] != 3 * side * side:
         raise ValueError("tokens: expected a contiguous [total, 3*side*side]")
     m, s = (ctypes.c_float * 3)(*mean), (ctypes.c_float * 3)(*stdv)

@@ -651,7 +651,8 @@ __device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, co
 /* Gradients of the queries: as the forward, 32 queries a wave, over the keys.  Where the keys are few (two
  * tiles at most), delta is summed up from weights and products here rather than taken from the narrowed
  * results, whose rounding weighs most there (in fp16, images of 5 tokens: gradients off by 3e-4 instead of 6e-4,
- * of 500 tokens 2.9e-4 instead of 3.0e-4); for the first tokens under a causal mask too. */
+ * of 500 tokens 2.9e-4 instead of 3.0e-4); for the first tokens under a causal mask too.  A bias by distance leaves a
+ * query few keys of weight however many there are: there the sum is a pass of its own over all keys. */
 constexpr int kExactSteps = 2;
 
 template <typename T, int DB, bool CAP, bool SLOPES>
@@ -695,17 +696,17 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
     const int steps = (all + kKeys - 1) / kKeys, plain = whole / kKeys;
     const int begin = steps <= kExactSteps ? (split ? steps : 0) : (int)((int64_t)steps * split / a.q_splits);
     const int end = steps <= kExactSteps ? steps : (int)((int64_t)steps * (split + 1) / a.q_splits);
-    const auto fetch = [&](int i) {
-        if (i >= end) return;
+    const auto fetch = [&](int i, int limit) {
+        if (i >= limit) return;
         fetch_k(tile(i & 1, 0), k + (int64_t)i * kKeys * a.k.token, p.m - i * kKeys, threadIdx.x);
         fetch_v(tile(i & 1, 1), v + (int64_t)i * kKeys * a.v.token, p.m - i * kKeys, threadIdx.x);
     };
-    fetch(begin);
+    float sum = 0.0f;
     if (steps <= kExactSteps) {
-        fetch(begin + 1);
+        fetch(begin, end);
+        fetch(begin + 1, end);
         fetched();
         __syncthreads();
-        float sum = 0.0f;
         for (int i = begin; i < end; ++i)
             q_grad_tile<T, DB, CAP, SLOPES, true, true>(grad, sum, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
         delta = across_sum(sum);
@@ -713,17 +714,30 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_q_grad_kernel(Backwa
         for (int i = begin; i < end; ++i)
             q_grad_tile<T, DB, CAP, SLOPES, true, false>(grad, delta, q, g, reader, tile(i, 0), tile(i, 1), i * kKeys, seen, place, lse2, score, lane);
     } else {
+        if (SLOPES) {
+            fetch(0, steps);
+            for (int i = 0; i < steps; ++i) {
+                fetched();
+                __syncthreads();
+                fetch(i + 1, steps);
+                q_grad_tile<T, DB, CAP, SLOPES, true, true>(grad, sum, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
+            }
+            delta = across_sum(sum);
+            if (row < p.n && half == 0 && split == 0) stats[1] = delta;
+            __syncthreads();
+        }
+        fetch(begin, end);
         int i = begin;
         for (; i < min(plain, end); ++i) {
             fetched();
             __syncthreads();
-            fetch(i + 1);
+            fetch(i + 1, end);
             q_grad_tile<T, DB, CAP, SLOPES, false, false>(grad, delta, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
         }
         for (; i < end; ++i) {
             fetched();
             __syncthreads();
-            fetch(i + 1);
+            fetch(i + 1, end);
             q_grad_tile<T, DB, CAP, SLOPES, true, false>(grad, delta, q, g, reader, tile(i & 1, 0), tile(i & 1, 1), i * kKeys, seen, place, lse2, score, lane);
         }
     }
