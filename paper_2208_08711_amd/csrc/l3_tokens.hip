@@ -555,14 +555,14 @@ void launch_rotate(const RotateArgs& a, int mode, unsigned grid, hipStream_t str
     const dim3 threads(kRotateThreads);
     if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
     else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
-    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, PER_SLOT>), dim3(grid), threads, 0, stream, a);
+    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, (PER_SLOT > 1 ? 2 : 1)>), dim3(grid), threads, 0, stream, a);
 }
 
 template <typename T>
 void launch_rotate(const RotateArgs& a, int v, int per_slot, int mode, unsigned grid, hipStream_t stream) {
-    if (v == 8 && per_slot == 4) launch_rotate<T, 8, 4>(a, mode, grid, stream);
+    if (v == 8 && per_slot > 1) launch_rotate<T, 8, 4>(a, mode, grid, stream);
     else if (v == 8) launch_rotate<T, 8, 1>(a, mode, grid, stream);
-    else if (v == 4 && per_slot == 4) launch_rotate<T, 4, 4>(a, mode, grid, stream);
+    else if (v == 4 && per_slot > 1) launch_rotate<T, 4, 4>(a, mode, grid, stream);
     else if (v == 4) launch_rotate<T, 4, 1>(a, mode, grid, stream);
     else launch_rotate<T, 1, 1>(a, mode, grid, stream);
 }
@@ -641,7 +641,7 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     if (rot->pairs) std::memcpy(a.turns, rot->turns, (size_t)rot->pairs * 8);
     /* Four heads a slot, where one of them each would still give all CUs their threads */
     const int64_t heads = side[0].heads + side[1].heads;
-    const int per_slot = v > 1 && a.tokens * heads * a.lanes >= kManyThreads ? 4 : 1;
+    const int per_slot = v > 1 && a.tokens * heads * a.lanes >= kManyThreads ? (mode == kNormRotateBack ? 2 : 4) : 1;
     a.q_slots = (side[0].heads + per_slot - 1) / per_slot;
     a.slots = std::max(1, a.q_slots + (side[1].heads + per_slot - 1) / per_slot);
     /* whole tokens: the launch's slots are a multiple of a token's */
