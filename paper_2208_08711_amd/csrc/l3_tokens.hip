@@ -555,7 +555,7 @@ void launch_rotate(const RotateArgs& a, int mode, unsigned grid, hipStream_t str
     const dim3 threads(kRotateThreads);
     if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
     else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
-    else hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, (PER_SLOT > 1 ? 2 : 1)>), dim3(grid), threads, 0, stream, a);
+    else if constexpr (V < 8) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, (PER_SLOT > 1 ? 2 : 1)>), dim3(grid), threads, 0, stream, a);
 }
 
 template <typename T>
@@ -601,7 +601,9 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     if (!work && mode != kNormRotateBack) return L3_OK;
 
     RotateArgs a = {};
-    int v = 8;
+    /* (the gradients keep three times as much a pair: at 8 pairs a lane two waves a SIMD have room, 81 us for 19683 tokens
+     * x 18 heads x 128, at 4 four, 61; their heads a slot 4 instead of 2: 91) */
+    int v = mode == kNormRotateBack ? 4 : 8;
     for (;; v = v == 8 ? 4 : 1) {
         if (v == 1) break;
         bool ok = rot->pairs / rot->axes % v == 0 && head_dim / 2 % v == 0;
