@@ -399,7 +399,7 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
     uint64_t turns[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) turns[i] = turned ? a.turns[j0 + i] : 0u;
-    const int axis = a.axes == 2 && j0 >= a.pairs / 2 ? 1 : 0;    /* V divides pairs/axes */
+    const int second = a.axes == 2 ? a.pairs / 2 - j0 : V;     /* of the lane's pairs, those from here on go by the second position */
     const float magnitude = turned ? a.magnitude : 1.0f, by_dim = 1.0f / (float)a.head_dim;
     float w[2][V], sum[2][V] = {};                             /* weights; backward: their gradients */
     if (MODE != kRotate) {
@@ -427,12 +427,16 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
             }
         }
         float cs[V], sn[V];
-        const int64_t position = turned ? (int64_t)a.positions[token * a.axes + axis] : 0;
+        int64_t positions[2] = {};
+        if (turned) {
+            positions[0] = a.positions[token * a.axes];
+            positions[1] = a.positions[token * a.axes + a.axes - 1];
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             /* the product wraps at whole turns; its high half as a signed fraction of a turn is what
              * the sine and cosine instructions take */
-            const uint64_t angle = (uint64_t)position * turns[i];
+            const uint64_t angle = (uint64_t)positions[i >= second] * turns[i];
             const float f = (float)(int32_t)(angle >> 32) * 0x1p-32f;
             cs[i] = __builtin_amdgcn_cosf(f) * magnitude;
             sn[i] = __builtin_amdgcn_sinf(f) * magnitude;
@@ -501,53 +505,51 @@ __global__ __launch_bounds__(kRotateThreads) void l3_rotate_kernel(RotateArgs a)
     }
 
     if (MODE == kNormRotateBack) {
-        /* every thread's sums into local memory, then those of one element top to bottom, the queries'
-         * and the keys' apart */
-        __shared__ float room[kRotateThreads * 2];
-        __shared__ uint8_t of_keys[kRotateThreads];
-        const int groups = kRotateThreads / a.lanes;
-        if (lane == 0) of_keys[threadIdx.x / a.lanes] = (uint8_t)which;
-        for (int i = 0; i < V; ++i) {
-            __syncthreads();
-            room[threadIdx.x * 2] = sum[0][i];
-            room[threadIdx.x * 2 + 1] = sum[1][i];
-            __syncthreads();
-            if ((int)threadIdx.x < a.lanes && active) {
-                float s[2][2] = {};
-                for (int g = 0; g < groups; ++g) {
-                    const float s0 = room[(g * a.lanes + lane) * 2], s1 = room[(g * a.lanes + lane) * 2 + 1];
-                    const bool k = of_keys[g];
-                    s[0][0] += k ? 0.0f : s0;
-                    s[0][1] += k ? 0.0f : s1;
-                    s[1][0] += k ? s0 : 0.0f;
-                    s[1][1] += k ? s1 : 0.0f;
+        /* the sums of one element within each wave, the queries' and the keys' apart, then of the waves in order */
+        __shared__ float room[kRotateThreads / 64][2][L3_MAX_HEAD_DIM];
+        const int wave = threadIdx.x / 64;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float s[2] = {which == k ? sum[0][i] : 0.0f, which == k ? sum[1][i] : 0.0f};
+                for (int d = a.lanes; d < 64; d <<= 1) {
+                    s[0] += __shfl_xor(s[0], d);
+                    s[1] += __shfl_xor(s[1], d);
                 }
-                for (int k = 0; k < 2; ++k) {
-                    float* const out = a.partial + ((int64_t)blockIdx.x * 2 + k) * a.head_dim;
-                    out[side_by_side ? 2 * (j0 + i) : j0 + i] = s[k][0];
-                    out[side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] = s[k][1];
+                if ((int)(threadIdx.x & 63) < a.lanes && active) {
+                    room[wave][k][side_by_side ? 2 * (j0 + i) : j0 + i] = s[0];
+                    room[wave][k][side_by_side ? 2 * (j0 + i) + 1 : j0 + i + a.pairs] = s[1];
                 }
             }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 2 * a.head_dim; e += kRotateThreads) {
+            const int k = e >= a.head_dim, c = k ? e - a.head_dim : e;
+            float s = room[0][k][c];
+#pragma unroll
+            for (int w = 1; w < kRotateThreads / 64; ++w) s += room[w][k][c];
+            a.partial[(int64_t)blockIdx.x * 2 * a.head_dim + e] = s;
         }
     }
 }
 
-/* Columns of the partial sums: one workgroup per element of one weight. */
+/* Columns of the partial sums: kColumns elements of the weights a workgroup, their rows shared out among
+ * its threads and joined in order. */
+constexpr int kColumns = 4;
 __global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const float* partial, int blocks, int head_dim, float* q, float* k) {
-    __shared__ float room[kRotateThreads];
-    const int column = blockIdx.x;
+    constexpr int kRows = kRotateThreads / kColumns;
+    __shared__ float room[kRows][kColumns];
+    const int c = threadIdx.x % kColumns, r = threadIdx.x / kColumns, column = blockIdx.x * kColumns + c;
     float s = 0.0f;
-    for (int b = threadIdx.x; b < blocks; b += kRotateThreads) s += partial[(int64_t)b * 2 * head_dim + column];
-    room[threadIdx.x] = s;
+    if (column < 2 * head_dim)
+#pragma unroll 16
+        for (int b = r; b < blocks; b += kRows) s += partial[(int64_t)b * 2 * head_dim + column];
+    room[r][c] = s;
     __syncthreads();
-    for (int n = kRotateThreads / 2; n > 0; n >>= 1) {
-        if ((int)threadIdx.x < n) room[threadIdx.x] += room[threadIdx.x + n];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-        float* const to = column < head_dim ? q : k;
-        if (to) to[column < head_dim ? column : column - head_dim] = room[0];
-    }
+    if (r || column >= 2 * head_dim) return;
+    for (int i = 1; i < kRows; ++i) s += room[i][c];
+    float* const to = column < head_dim ? q : k;
+    if (to) to[column < head_dim ? column : column - head_dim] = s;
 }
 
 template <typename T, int V, int PER_SLOT>
@@ -606,7 +608,7 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     int v = mode == kNormRotateBack ? 4 : 8;
     for (;; v = v == 8 ? 4 : 1) {
         if (v == 1) break;
-        bool ok = rot->pairs / rot->axes % v == 0 && head_dim / 2 % v == 0;
+        bool ok = rot->pairs % v == 0 && head_dim / 2 % v == 0;
         for (int s = 0; s < 2; ++s)
             if (side[s].heads)
                 ok = ok && wide_heads(side[s].x, v) && wide_heads(side[s].y, v) &&
@@ -662,7 +664,7 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     else if (grid) launch_rotate<_Float16>(a, v, per_slot, mode, (unsigned)grid, st);
     if (mode == kNormRotateBack) {
         if (launched() != L3_OK) return L3_ERR_DEVICE;
-        hipLaunchKernelGGL(l3_weight_grad_kernel, dim3((unsigned)(2 * head_dim)), dim3(kRotateThreads), 0, st, partial, (int)grid,
+        hipLaunchKernelGGL(l3_weight_grad_kernel, dim3((unsigned)((2 * head_dim + kColumns - 1) / kColumns)), dim3(kRotateThreads), 0, st, partial, (int)grid,
                            head_dim, q_weight_grad, k_weight_grad);
     }
     return launched();
