@@ -51,7 +51,7 @@ typedef struct {
  *   d_first      DEVICE int32 [n+1] or NULL: each image's first token, then the number of tokens
  *   tokens       how many tokens d_tokens has room for: must be what l3_patch_tokens_count gives
  * Errors: INVALID_ARG (also: zero sizes, a stride too small, `tokens` wrong, unaligned d_tokens,
- * zero stdv), LIMIT (2^31 tokens or more), DEVICE. */
+ * zero stdv), LIMIT (2^31 tokens or more, 2^28 pixels or more in a row or column), DEVICE. */
 l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n, uint32_t side,
                                 const float mean[3], const float stdv[3], l3_dtype dtype,
                                 void* d_tokens, int64_t tokens, int32_t* d_positions, int32_t* d_first,
@@ -174,7 +174,7 @@ typedef struct {
     l3_mask        mask;
     const int32_t* d_prefix;             /* DEVICE [images], for L3_MASK_PREFIX */
     float          scale;
-    float          cap;                  /* 0: none */
+    float          cap;                  /* 0: none (scale / cap within the range of float) */
     const float*   d_slopes;             /* DEVICE [q_heads] or NULL */
     l3_dtype       dtype;
 } l3_attention_shape;

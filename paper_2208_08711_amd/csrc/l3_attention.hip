@@ -1051,7 +1051,7 @@ __global__ __launch_bounds__(L3_MAX_HEAD_DIM) void l3_attention_join_kernel(Step
 
 /* ---- host ---------------------------------------------------------------------------------- */
 
-l3_status launched() { return hipGetLastError() == hipSuccess ? L3_OK : L3_ERR_DEVICE; }
+l3_status status_of(bool launched) { return launched ? L3_OK : L3_ERR_DEVICE; }
 bool known(l3_dtype dtype) { return dtype == L3_BF16 || dtype == L3_FP16; }
 bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 bool good_heads(const l3_heads& h) {
@@ -1061,7 +1061,8 @@ Heads heads_of(const l3_heads& h) { return {h.d, h.token_stride, h.head_stride};
 
 bool good_numbers(int head_dim, int q_heads, int kv_heads, float scale, float cap) {
     return head_dim >= 8 && head_dim <= L3_MAX_HEAD_DIM && head_dim % 8 == 0 && q_heads >= 1 && kv_heads >= 1 &&
-           q_heads % kv_heads == 0 && scale >= 0.0f && std::isfinite(scale) && cap >= 0.0f && std::isfinite(cap);
+           q_heads % kv_heads == 0 && scale >= 0.0f && std::isfinite(scale) && cap >= 0.0f && std::isfinite(cap) &&
+           (cap == 0.0f || std::isfinite(4.0f * scale / cap));
 }
 
 /* Rows of a tile are reached by 32-bit offsets. */
@@ -1119,15 +1120,14 @@ l3_status run_forward(const ForwardArgs& a, hipStream_t stream) {
     if (grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
     const bool few = few_queries(a.s, grid);
     if (few) grid = most_tiles(a.s.q_tokens, a.s.images, 32) * a.s.q_heads;
+    bool ok = false;
     by_width(a.s.head_dim, [&](auto db) {
         by_score(a.s.cap > 0.0f, a.s.slopes != nullptr, [&](auto cap, auto slopes) {
-            if (few)
-                hipLaunchKernelGGL((l3_attention_few_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
-            else
-                hipLaunchKernelGGL((l3_attention_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+            ok = launch(few ? l3_attention_few_kernel<T, db.value, cap.value, slopes.value> : l3_attention_kernel<T, db.value, cap.value, slopes.value>, grid,
+                        kThreads, 0, stream, a);
         });
     });
-    return launched();
+    return status_of(ok);
 }
 
 /* How the gradients are split.  Workgroups that share a tile of keys: of the query heads that share it as few
@@ -1180,27 +1180,21 @@ l3_status run_backward(const BackwardArgs& a, hipStream_t stream) {
     const int64_t kv_join = splits > 1 ? blocks((int64_t)s.kv_tokens * s.kv_heads * s.head_dim / 4) : 0;
     for (const int64_t grid : {q_grid, kv_grid, stats_grid, q_join, kv_join})
         if (grid >= (int64_t)1 << 31) return L3_ERR_LIMIT;
-    if (stats_grid) hipLaunchKernelGGL((l3_attention_stats_kernel<T>), dim3((unsigned)stats_grid), dim3(kThreads), 0, stream, a);
-    if (launched() != L3_OK) return L3_ERR_DEVICE;
+    bool ok = !stats_grid || launch(l3_attention_stats_kernel<T>, stats_grid, kThreads, 0, stream, a);
     by_width(s.head_dim, [&](auto db) {
         by_score(s.cap > 0.0f, s.slopes != nullptr, [&](auto cap, auto slopes) {
             /* (queries first: they leave better deltas) */
-            if (q_grid)
-                hipLaunchKernelGGL((l3_attention_q_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)q_grid), dim3(kThreads), 0,
-                                   stream, a);
-            if (q_join)
-                hipLaunchKernelGGL((l3_attention_grad_join_kernel<T>), dim3((unsigned)q_join), dim3(kThreads), 0, stream, a.partial, a.q_splits,
-                                   s.q_first, s.images, s.q_tokens, s.q_heads, s.head_dim, a.q_grad, Heads{});
-            if (kv_grid)
-                hipLaunchKernelGGL((l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)kv_grid), dim3(kThreads), 0,
-                                   stream, a);
+            if (ok && q_grid) ok = launch(l3_attention_q_grad_kernel<T, db.value, cap.value, slopes.value>, q_grid, kThreads, 0, stream, a);
+            if (ok && q_join)
+                ok = launch(l3_attention_grad_join_kernel<T>, q_join, kThreads, 0, stream, a.partial, a.q_splits, s.q_first, s.images, s.q_tokens,
+                            s.q_heads, s.head_dim, a.q_grad, Heads{});
+            if (ok && kv_grid) ok = launch(l3_attention_kv_grad_kernel<T, db.value, cap.value, slopes.value>, kv_grid, kThreads, 0, stream, a);
         });
     });
-    if (launched() != L3_OK) return L3_ERR_DEVICE;
-    if (kv_join)
-        hipLaunchKernelGGL((l3_attention_grad_join_kernel<T>), dim3((unsigned)kv_join), dim3(kThreads), 0, stream, a.partial, splits, s.kv_first, s.images,
-                           s.kv_tokens, s.kv_heads, s.head_dim, a.k_grad, a.v_grad);
-    return launched();
+    if (ok && kv_join)
+        ok = launch(l3_attention_grad_join_kernel<T>, kv_join, kThreads, 0, stream, a.partial, splits, s.kv_first, s.images, s.kv_tokens, s.kv_heads,
+                    s.head_dim, a.k_grad, a.v_grad);
+    return status_of(ok);
 }
 
 /* How the caches are cut: chunks of whole rounds of the waves, so many that every CU has a few
@@ -1216,15 +1210,14 @@ template <typename T>
 l3_status run_step(const StepArgs& a, hipStream_t stream) {
     const int64_t grid = (int64_t)a.n * a.kv_heads * a.blocks_of_heads * a.chunks;
     if (grid >= (int64_t)1 << 31 || (int64_t)a.n * a.q_heads >= (int64_t)1 << 31) return L3_ERR_LIMIT;
+    bool ok = false;
     by_width(a.head_dim, [&](auto db) {
         by_score(a.cap > 0.0f, a.slopes != nullptr, [&](auto cap, auto slopes) {
-            hipLaunchKernelGGL((l3_attention_step_kernel<T, db.value, cap.value, slopes.value>), dim3((unsigned)grid), dim3(kStepThreads), 0,
-                               stream, a);
+            ok = launch(l3_attention_step_kernel<T, db.value, cap.value, slopes.value>, grid, kStepThreads, 0, stream, a);
         });
     });
-    if (launched() != L3_OK) return L3_ERR_DEVICE;
-    if (a.partial) hipLaunchKernelGGL((l3_attention_join_kernel<T>), dim3((unsigned)(a.n * a.q_heads)), dim3(L3_MAX_HEAD_DIM), 0, stream, a);
-    return launched();
+    if (ok && a.partial) ok = launch(l3_attention_join_kernel<T>, (int64_t)a.n * a.q_heads, L3_MAX_HEAD_DIM, 0, stream, a);
+    return status_of(ok);
 }
 
 }  // namespace

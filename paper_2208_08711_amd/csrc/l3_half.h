@@ -8,6 +8,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <tuple>
+#include <utility>
+
 namespace {
 
 template <typename T, int N> struct HalfVec { typedef T type __attribute__((ext_vector_type(N))); };
@@ -36,6 +39,17 @@ __device__ __forceinline__ void store_narrow(T* p, const float (&in)[N]) {
         for (int i = 0; i < N; ++i) f[i] = in[i];
         *reinterpret_cast<typename HalfVec<T, N>::type*>(p) = __builtin_convertvector(f, typename HalfVec<T, N>::type);
     }
+}
+
+/* Launches and says whether that went well, whatever errors of others the runtime still remembers. */
+template <typename... P, size_t... I>
+bool launch_held(void (*kernel)(P...), unsigned grid, unsigned threads, size_t lds, hipStream_t stream, std::tuple<P...> held, std::index_sequence<I...>) {
+    void* args[] = {&std::get<I>(held)...};
+    return hipLaunchKernel((const void*)kernel, dim3(grid), dim3(threads), args, lds, stream) == hipSuccess;
+}
+template <typename... P, typename... A>
+bool launch(void (*kernel)(P...), int64_t grid, unsigned threads, size_t lds, hipStream_t stream, const A&... args) {
+    return launch_held(kernel, (unsigned)grid, threads, lds, stream, std::tuple<P...>(args...), std::index_sequence_for<P...>());
 }
 
 }  // namespace

@@ -14,7 +14,7 @@
 
 namespace {
 
-l3_status launched() { return hipGetLastError() == hipSuccess ? L3_OK : L3_ERR_DEVICE; }
+l3_status status_of(bool launched) { return launched ? L3_OK : L3_ERR_DEVICE; }
 
 bool known(l3_dtype dtype) { return dtype == L3_BF16 || dtype == L3_FP16; }
 
@@ -37,6 +37,8 @@ typedef u32x3 u32x3_any __attribute__((aligned(1)));
 constexpr int kTokenThreads = 256;
 constexpr uint32_t kStripBytes = 24576;
 constexpr uint32_t kTokenImages = 64;      /* descriptors in the arguments of one launch */
+
+constexpr uint32_t kMostPixels = 1u << 28; /* of a side of an image: places in a row are 32-bit numbers */
 
 struct TokenImage {
     const uint8_t* rgb;
@@ -238,8 +240,8 @@ struct DropoutArgs {
 
 constexpr int kDropoutThreads = 256;
 
-/* One lane, one counter block: 8 consecutive elements.  WIDE: the rows lie end to end in every
- * tensor (rows is 1 then) and all are 16-byte aligned. */
+/* One lane, one counter block: 8 consecutive elements.  WIDE: all eight lie side by side, 16-byte aligned, in
+ * every tensor (but for those behind the end): one row, or rows of a multiple of eight. */
 template <typename T, bool WIDE, bool RESIDUAL>
 __global__ __launch_bounds__(kDropoutThreads) void l3_dropout_kernel(DropoutArgs a) {
     const int64_t count = a.rows * a.cols, blocks = (count + 7) / 8;
@@ -248,9 +250,14 @@ __global__ __launch_bounds__(kDropoutThreads) void l3_dropout_kernel(DropoutArgs
         const int64_t e0 = b * 8;
         const bool whole = WIDE && e0 + 8 <= count;
         float x[8], z[8] = {};
+        int64_t row = 0, col = e0;
+        if (!WIDE || a.rows > 1) {
+            row = count < (int64_t)1 << 31 ? (int64_t)((uint32_t)e0 / (uint32_t)a.cols) : e0 / a.cols;
+            col = e0 - row * a.cols;
+        }
         if (whole) {
-            load_wide<T, 8>((const T*)a.x + e0, x);
-            if (RESIDUAL) load_wide<T, 8>((const T*)a.residual + e0, z);
+            load_wide<T, 8>((const T*)a.x + row * a.x_stride + col, x);
+            if (RESIDUAL) load_wide<T, 8>((const T*)a.residual + row * a.residual_stride + col, z);
         }
         const Philox random = philox((uint64_t)b, offset, a.seed);
         if (whole) {
@@ -259,10 +266,9 @@ __global__ __launch_bounds__(kDropoutThreads) void l3_dropout_kernel(DropoutArgs
                 const uint32_t bits = (random.w[i / 2] >> (16 * (i & 1))) & 0xFFFFu;
                 z[i] += bits >= a.threshold ? x[i] * a.scale : 0.0f;
             }
-            store_narrow<T, 8>((T*)a.y + e0, z);
+            store_narrow<T, 8>((T*)a.y + row * a.y_stride + col, z);
             continue;
         }
-        int64_t row = e0 / a.cols, col = e0 - row * a.cols;
         const int n = (int)min((int64_t)8, count - e0);
         for (int i = 0; i < n; ++i) {
             const uint32_t word = i < 4 ? (i < 2 ? random.w[0] : random.w[1]) : (i < 6 ? random.w[2] : random.w[3]);
@@ -280,16 +286,10 @@ __global__ __launch_bounds__(kDropoutThreads) void l3_dropout_kernel(DropoutArgs
 
 template <typename T>
 l3_status launch_dropout(const DropoutArgs& a, bool wide, hipStream_t stream) {
-    const int64_t blocks = (a.rows * a.cols + 8 * kDropoutThreads - 1) / (8 * kDropoutThreads);
-    const dim3 grid((unsigned)std::min<int64_t>(blocks, 256 * 32)), threads(kDropoutThreads);
-    if (a.residual) {
-        if (wide) hipLaunchKernelGGL((l3_dropout_kernel<T, true, true>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((l3_dropout_kernel<T, false, true>), grid, threads, 0, stream, a);
-    } else {
-        if (wide) hipLaunchKernelGGL((l3_dropout_kernel<T, true, false>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((l3_dropout_kernel<T, false, false>), grid, threads, 0, stream, a);
-    }
-    return launched();
+    const int64_t blocks = (a.rows * a.cols + 8 * kDropoutThreads - 1) / (8 * kDropoutThreads), grid = std::min<int64_t>(blocks, 256 * 32);
+    const auto kernel = a.residual ? (wide ? l3_dropout_kernel<T, true, true> : l3_dropout_kernel<T, false, true>)
+                                   : (wide ? l3_dropout_kernel<T, true, false> : l3_dropout_kernel<T, false, false>);
+    return status_of(launch(kernel, grid, kDropoutThreads, 0, stream, a));
 }
 
 /* ------------------------------------------------------------------------
@@ -553,20 +553,18 @@ __global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const fl
 }
 
 template <typename T, int V, int PER_SLOT>
-void launch_rotate(const RotateArgs& a, int mode, unsigned grid, hipStream_t stream) {
-    const dim3 threads(kRotateThreads);
-    if (mode == kRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
-    else if (mode == kNormRotate) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotate, PER_SLOT>), dim3(grid), threads, 0, stream, a);
-    else if constexpr (V < 8) hipLaunchKernelGGL((l3_rotate_kernel<T, V, kNormRotateBack, (PER_SLOT > 1 ? 2 : 1)>), dim3(grid), threads, 0, stream, a);
+bool launch_rotate(const RotateArgs& a, int mode, int64_t grid, hipStream_t stream) {
+    if (mode == kRotate) return launch(l3_rotate_kernel<T, V, kRotate, PER_SLOT>, grid, kRotateThreads, 0, stream, a);
+    if (mode == kNormRotate) return launch(l3_rotate_kernel<T, V, kNormRotate, PER_SLOT>, grid, kRotateThreads, 0, stream, a);
+    if constexpr (V < 8) return launch(l3_rotate_kernel<T, V, kNormRotateBack, (PER_SLOT > 1 ? 2 : 1)>, grid, kRotateThreads, 0, stream, a);
+    return false;
 }
 
 template <typename T>
-void launch_rotate(const RotateArgs& a, int v, int per_slot, int mode, unsigned grid, hipStream_t stream) {
-    if (v == 8 && per_slot > 1) launch_rotate<T, 8, 4>(a, mode, grid, stream);
-    else if (v == 8) launch_rotate<T, 8, 1>(a, mode, grid, stream);
-    else if (v == 4 && per_slot > 1) launch_rotate<T, 4, 4>(a, mode, grid, stream);
-    else if (v == 4) launch_rotate<T, 4, 1>(a, mode, grid, stream);
-    else launch_rotate<T, 1, 1>(a, mode, grid, stream);
+bool launch_rotate(const RotateArgs& a, int v, int per_slot, int mode, int64_t grid, hipStream_t stream) {
+    if (v == 8) return per_slot > 1 ? launch_rotate<T, 8, 4>(a, mode, grid, stream) : launch_rotate<T, 8, 1>(a, mode, grid, stream);
+    if (v == 4) return per_slot > 1 ? launch_rotate<T, 4, 4>(a, mode, grid, stream) : launch_rotate<T, 4, 1>(a, mode, grid, stream);
+    return launch_rotate<T, 1, 1>(a, mode, grid, stream);
 }
 
 bool good_heads(const l3_heads& h) { return h.d && aligned(h.d, 2) && h.token_stride >= 0 && h.head_stride >= 0; }
@@ -660,14 +658,13 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     const hipStream_t st = (hipStream_t)stream;
-    if (grid && dtype == L3_BF16) launch_rotate<__bf16>(a, v, per_slot, mode, (unsigned)grid, st);
-    else if (grid) launch_rotate<_Float16>(a, v, per_slot, mode, (unsigned)grid, st);
-    if (mode == kNormRotateBack) {
-        if (launched() != L3_OK) return L3_ERR_DEVICE;
-        hipLaunchKernelGGL(l3_weight_grad_kernel, dim3((unsigned)((2 * head_dim + kColumns - 1) / kColumns)), dim3(kRotateThreads), 0, st, partial, (int)grid,
-                           head_dim, q_weight_grad, k_weight_grad);
-    }
-    return launched();
+    bool ok = true;
+    if (grid)
+        ok = dtype == L3_BF16 ? launch_rotate<__bf16>(a, v, per_slot, mode, grid, st) : launch_rotate<_Float16>(a, v, per_slot, mode, grid, st);
+    if (ok && mode == kNormRotateBack)
+        ok = launch(l3_weight_grad_kernel, (2 * head_dim + kColumns - 1) / kColumns, kRotateThreads, 0, st, partial, (int)grid, head_dim, q_weight_grad,
+                    k_weight_grad);
+    return status_of(ok);
 }
 
 }  // namespace
@@ -692,6 +689,7 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
     for (int i = 0; i < n; ++i) {
         const l3_token_image& im = images[i];
         if (!im.d_rgb || !im.width || !im.height || im.row_stride < 3 * (uint64_t)im.width) return L3_ERR_INVALID_ARG;
+        if (im.width >= kMostPixels || im.height >= kMostPixels) too_many = true;
         const int64_t count = l3_patch_tokens_count(im.width, im.height, side);
         too_many = too_many || count >= (int64_t)1 << 31 || total + count >= (int64_t)1 << 31;
         if (!too_many) total += count;
@@ -727,8 +725,7 @@ l3_status l3_patch_tokens_batch(l3_ctx* ctx, const l3_token_image* images, int n
             first += cols * rows;
         }
         for (uint32_t i = a.images; i < kTokenImages; ++i) a.image[i] = {};
-        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kTokenThreads), lds, (hipStream_t)stream, a);
-        if (launched() != L3_OK) return L3_ERR_DEVICE;
+        if (!launch(kernel, blocks, kTokenThreads, lds, (hipStream_t)stream, a)) return L3_ERR_DEVICE;
     }
     return L3_OK;
 }
@@ -750,7 +747,8 @@ l3_status l3_dropout(l3_ctx* ctx, const void* d_x, int64_t x_stride, const void*
         a.cols = rows * cols;
         a.rows = 1;
     }
-    const bool wide = a.rows == 1 && aligned(d_x, 16) && aligned(d_y, 16) && aligned(d_residual, 16);
+    const bool rows_wide = a.rows == 1 || (cols % 8 == 0 && x_stride % 8 == 0 && y_stride % 8 == 0 && (!d_residual || residual_stride % 8 == 0));
+    const bool wide = rows_wide && aligned(d_x, 16) && aligned(d_y, 16) && aligned(d_residual, 16);
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return L3_ERR_DEVICE;
     return dtype == L3_BF16 ? launch_dropout<__bf16>(a, wide, (hipStream_t)stream) : launch_dropout<_Float16>(a, wide, (hipStream_t)stream);

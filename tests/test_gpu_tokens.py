@@ -103,7 +103,7 @@ def test_patch_tokens_many_images_and_a_wide_one(l3, ctx):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols", ((1, 1), (1, 7), (1, 8), (3, 5), (4, 64), (17, 129), (300, 1000)))
-@pytest.mark.parametrize("layout", ("flat", "apart", "odd"))
+@pytest.mark.parametrize("layout", ("flat", "apart", "wide rows", "odd"))
 @pytest.mark.parametrize("residual", (False, True))
 def test_dropout(l3, ctx, rows, cols, layout, residual, dtype):
     p, seed, offset = 0.3, 0xFEDCBA9876543210, 2 ** 40 + 5
@@ -113,6 +113,10 @@ def test_dropout(l3, ctx, rows, cols, layout, residual, dtype):
     guard = None
     if layout == "apart":
         wide = [torch.full((rows, cols + 3), 5.0, dtype=dtype, device="cuda") for _ in range(3)]
+        wide[0][:, :cols], wide[1][:, :cols] = x, z
+        x, z, out, guard = wide[0][:, :cols], wide[1][:, :cols], wide[2][:, :cols], wide[2][:, cols:]
+    elif layout == "wide rows":                                         # aligned rows apart
+        wide = [torch.full((rows, (cols + 15) // 8 * 8), 5.0, dtype=dtype, device="cuda") for _ in range(3)]
         wide[0][:, :cols], wide[1][:, :cols] = x, z
         x, z, out, guard = wide[0][:, :cols], wide[1][:, :cols], wide[2][:, :cols], wide[2][:, cols:]
     elif layout == "odd":
@@ -430,6 +434,21 @@ def test_attention_infinities(l3, ctx):
     ref.close(out[keep, 0], want, (ref.half(torch.bfloat16) + 2 * ref.SLACK) * (w @ v[others, 0].cpu().double().abs()), "out")
     assert bool(out[20].isnan().all())
     assert bool((out[50:, 0, 5] == math.inf).all()) and bool(out[50:, 0, :5].isfinite().all()) and bool(out[50:, 0, 6:].isfinite().all())
+
+
+def test_attention_without_keys_or_queries(l3, ctx):
+    """No keys at all: zeros, and no gradient for the queries; no queries at all: none for keys and values."""
+    some, none = normal((40, 2, 64), 36, torch.bfloat16), torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    a, z = torch.tensor([0, 40], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    out, lse, grads = torch.full_like(some, 3.0), torch.full((2, 40), 3.0, device="cuda"), torch.full_like(some, 3.0)
+    l3.attention(ctx, some, none, none, out, a, kv_first=z, lse=lse)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    l3.attention_backward(ctx, some, none, none, out, lse, some, grads, none.clone(), none.clone(), a, kv_first=z)
+    assert bool((grads == 0).all())
+    k_grad, v_grad, empty = torch.full_like(some, 3.0), torch.full_like(some, 3.0), torch.empty((2, 0), device="cuda")
+    l3.attention(ctx, none, some, some, none.clone(), z, kv_first=a, lse=empty)
+    l3.attention_backward(ctx, none, some, some, none, empty, none, none.clone(), k_grad, v_grad, z, kv_first=a)
+    assert bool((k_grad == 0).all()) and bool((v_grad == 0).all())
 
 
 def test_attention_scale_of_zero(l3, ctx):

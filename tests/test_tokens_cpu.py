@@ -72,7 +72,8 @@ def test_patch_tokens_refusals(lib):
         (dict(images=image(height=0)), INVALID),
         (dict(images=image(stride=3 << 32, width=0xFFFFFFFF, height=0xFFFFFFFF), tokens=1 << 60), LIMIT),
         (dict(images=image(stride=3 << 17, width=1 << 17, height=1 << 14), side=1, tokens=1 << 31), LIMIT),
-        (dict(n=0, tokens=0), OK), (dict(n=0, images=None, tokens=0, d_tokens=None), OK), (dict(d_positions=None, d_first=None), DEVICE)])
+        (dict(images=image(stride=3 << 28, width=1 << 28, height=1), side=64, tokens=1 << 22), LIMIT),
+        (dict(images=image(height=1 << 28), side=64, tokens=1 << 23), LIMIT), (dict(n=0, tokens=0), OK), (dict(n=0, images=None, tokens=0, d_tokens=None), OK), (dict(d_positions=None, d_first=None), DEVICE)])
 
 
 def test_patch_tokens_count():
@@ -182,7 +183,7 @@ BAD_SHAPES = [(dict(head_dim=60), INVALID), (dict(head_dim=0), INVALID), (dict(h
               (dict(kv_tokens=-1, d_kv_first=A), INVALID), (dict(kv_tokens=99), INVALID), (dict(d_q_first=None), INVALID),
               (dict(d_q_first=A + 2), INVALID), (dict(d_kv_first=A + 2), INVALID), (dict(mask=3), INVALID), (dict(mask=2), INVALID),
               (dict(mask=2, d_prefix=A + 1), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID),
-              (dict(cap=-1.0), INVALID), (dict(cap=NAN), INVALID), (dict(d_slopes=A + 2), INVALID), (dict(dtype=2), INVALID),
+              (dict(cap=-1.0), INVALID), (dict(cap=1e-44), INVALID), (dict(cap=NAN), INVALID), (dict(d_slopes=A + 2), INVALID), (dict(dtype=2), INVALID),
               (dict(q_tokens=1 << 31, kv_tokens=1 << 31), LIMIT), (dict(q_heads=65536, kv_heads=1), LIMIT)]
 GOOD_SHAPES = [dict(mask=1), dict(mask=2, d_prefix=A), dict(cap=5.0), dict(d_slopes=A), dict(scale=0.0), dict(kv_tokens=7, d_kv_first=A), dict(head_dim=8)]
 
