@@ -6,6 +6,7 @@ CPU fallback: if libl3.so is missing, every call raises.
 """
 import array
 import ctypes
+import itertools
 import operator
 import os
 import sys
@@ -492,7 +493,8 @@ def patch_tokens_count(width, height, side):
 
 # patch_tokens_batch relies on this layout
 assert ctypes.sizeof(_TokenImage) == 24 and _TokenImage.width.offset == 16 and _TokenImage.height.offset == 20
-_stride, _get_device, _dtype = operator.methodcaller("stride"), operator.methodcaller("get_device"), operator.attrgetter("dtype")
+_stride, _get_device, _is_contiguous = map(operator.methodcaller, ("stride", "get_device", "is_contiguous"))
+_dtype = operator.attrgetter("dtype")
 
 
 def patch_tokens_batch(ctx, images, side, mean, stdv, tokens, positions=None, first=None, stream=None, row_strides=None):
@@ -506,8 +508,9 @@ def patch_tokens_batch(ctx, images, side, mean, stdv, tokens, positions=None, fi
     # the l3_token_image array, three words of 8 bytes each, filled column by column as in encode_batch
     # (256 photographs: 330 us image by image, a third so)
     words, sides, rows = array.array("Q", bytes(24 * n)), [], []
+    whole = all(map(_is_contiguous, images))                            # (cheaper to ask than all the strides)
     try:
-        for (h, w, c), (row, pixel, channel) in zip(map(_shape, images), map(_stride, images)):
+        for (h, w, c), (row, pixel, channel) in zip(map(_shape, images), itertools.repeat((0, 3, 1)) if whole else map(_stride, images)):
             if c != 3 or pixel != 3 or channel != 1:
                 raise ValueError
             sides.append(w & _MASK32 | (h & _MASK32) << 32)
