@@ -542,8 +542,13 @@ __global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const fl
     const int c = threadIdx.x % kColumns, r = threadIdx.x / kColumns, column = blockIdx.x * kColumns + c;
     float s = 0.0f;
     if (column < 2 * head_dim)
-#pragma unroll 16
-        for (int b = r; b < blocks; b += kRows) s += partial[(int64_t)b * 2 * head_dim + column];
+        for (int b = r; b < blocks; b += 8 * kRows) {
+            float part[8];                                         /* eight loads on the way together */
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[i] = b + i * kRows < blocks ? partial[(int64_t)(b + i * kRows) * 2 * head_dim + column] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += part[i];
+        }
     room[r][c] = s;
     __syncthreads();
     if (r || column >= 2 * head_dim) return;
