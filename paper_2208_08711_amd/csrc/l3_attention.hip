@@ -454,6 +454,14 @@ __device__ __forceinline__ void load_operand(typename HalfVec<T, 8>::type (&q)[2
 constexpr int kQueries = 128;              /* of a workgroup: 32 a wave */
 constexpr int kKeys = 64;                  /* of a tile */
 
+/* 128 queries of one image and head a workgroup, 32 a wave, past all keys that any of them sees, in tiles of 64
+ * with the next one on its way into the other half of the local memory (one barrier a tile).  Tiles that all see
+ * come first, without masks; a lane's vector work per score is one multiply-add, half a maximum, exponential,
+ * add and half a conversion, some 28 cycles against the matrix cores' 32 (64 wide) or 16 (128 wide: 32 of 64), so
+ * both pipes are close to each other and two waves a SIMD take turns: bound by issue, not by local memory (no
+ * bank conflicts, 60 % of its rate) nor memory.  4 x 8192 tokens, bf16: 16 heads 64 wide 1.17-1.27 ms, 865-940 TFLOP/s; 128
+ * wide 2.05-2.10 ms, 1050-1070 (a large library product on these cards: 1330); with a cap, causal, 1.36 ms against
+ * 1.09 (the hyperbolic tangent is two more of the slow instructions).  Raised wave priority around the products: no faster. */
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kThreads, 2) void l3_attention_kernel(ForwardArgs a) {
     __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kKeys * Tile<DB>::kPitch];
@@ -652,7 +660,9 @@ __device__ __forceinline__ void q_grad_tile(f32x16 (&grad)[DB], float& delta, co
  * tiles at most), delta is summed up from weights and products here rather than taken from the narrowed
  * results, whose rounding weighs most there (in fp16, images of 5 tokens: gradients off by 3e-4 instead of 6e-4,
  * of 500 tokens 2.9e-4 instead of 3.0e-4); for the first tokens under a causal mask too.  A bias by distance leaves a
- * query few keys of weight however many there are: there the sum is a pass of its own over all keys. */
+ * query few keys of weight however many there are: there the sum is a pass of its own over all keys.
+ * Bound as the forward is, at three products instead of two: 4 x 8192 tokens, bf16, 16 heads 64 wide 1.7 ms, 128 wide 2.8 ms
+ * (950 and 1170 TFLOP/s of its own products); causal and capped 1.8 (matrix cores 44 % busy, vector unit 64 %). */
 constexpr int kExactSteps = 2;
 
 template <typename T, int DB, bool CAP, bool SLOPES>
@@ -810,7 +820,12 @@ __device__ __forceinline__ void kv_grad_tile(f32x16 (&dk)[DB], f32x16 (&dv)[DB],
 
 /* Gradients of keys and values: 32 keys a wave (one a lane), over the queries of all heads that share
  * them (or, split, of some of these).  S = Q K^T gives a lane 16 queries of its key, and P and dS are second
- * operands of dV^T = dO^T P and dK^T = Q^T dS as they are. */
+ * operands of dV^T = dO^T P and dK^T = Q^T dS as they are.  Two kernels, this and the queries', work the scores out
+ * twice (seven products instead of five) so that no sum depends on the order in which workgroups finish.
+ * Registers decide: 128 sums, 32 scores and 32 of keys a lane at 128 wide leave no room for the values
+ * at two waves a SIMD: they are in local memory (four street scenes, causal and capped: one wave a SIMD 3.4 ms, two with
+ * 40 registers spilled 2.9, without 2.3).  4 x 8192 tokens, bf16, 16 heads on 2, 128 wide 4.1 ms (1070 TFLOP/s of its own
+ * products), causal 2.2, capped 2.5; 16 heads 64 wide 2.15 ms (1020). */
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(BackwardArgs a) {
     __shared__ __attribute__((aligned(256))) uint8_t tiles[2 * 2 * kBackQueries * Tile<DB>::kPitch];
@@ -896,6 +911,7 @@ __global__ __launch_bounds__(kThreads, 2) void l3_attention_kv_grad_kernel(Backw
                                                     (float)(begin + i * kBackQueries - from_key), score, lane);
         }
     }
+    fetched();                             /* (the values' tile, where there was no query) */
     if (key >= p.m) return;
     const int64_t row = p.k0 + key;
     T* const k_out = (T*)const_cast<void*>(a.k_grad.d) + row * a.k_grad.token + (int64_t)kv_head * a.k_grad.head;
@@ -969,7 +985,9 @@ struct StepArgs {
 };
 
 /* A workgroup takes `chunk` keys of one sequence and key head, against up to 32 of the query heads
- * that share them (one a lane); its waves take tiles in turn, each on its own, and join at the end. */
+ * that share them (one a lane); its waves take tiles in turn, each on its own, and join at the end.  Bound by
+ * memory: 32 caches of 512 to 32768 tokens x 8 heads x 128 (2.29 GB) in 440 us, 5.2 TB/s, what a copy reaches; with the
+ * heads' workgroups far apart in the launch 556 us (rows of 256 bytes 2 KB apart), in pieces four times as long 567. */
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(StepArgs a) {
     constexpr int kTile = kStepKeys * Tile<DB>::kPitch;

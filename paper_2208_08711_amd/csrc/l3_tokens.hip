@@ -28,7 +28,10 @@ bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) 
  * looks the values of their bytes up and puts them, channel by channel, where they belong in an image of the
  * output in local memory, RUN pixels of a patch's row at a time; from there whole lines go out, PIECE
  * elements at a time (a patch is a multiple of that).  RUN, PIECE: 4, 8 where 4 divides the side, 2, 4
- * for other even sides, else 1, 1. */
+ * for other even sides, else 1, 1.
+ * Twice as many bytes are written as read.  4 scenes of 2048x1024, side 16, bf16 (76 MB): 17 us, 4.4 TB/s; 256 photographs,
+ * side 14, fp16 (359 MB, four launches): 131 us, 2.7 TB/s, of which the launches' ends are some 20 (one image of 29 million
+ * pixels: 3.3 TB/s at 14, 3.5 at 16).  Gathering bytes for every element in the order of the output instead: 36 and 206 us. */
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
@@ -210,7 +213,9 @@ struct Philox {
     uint32_t w[4];
 };
 
-/* Philox 4x32 with 7 rounds (the fewest its authors found to pass every test of BigCrush). */
+/* Philox 4x32 with 7 rounds (the fewest its authors found to pass every test of BigCrush).  Sixteen bits an
+ * element make one call of 14 wide products serve 16 bytes, which hides behind the memory: 65536 x 1024 fp16
+ * with residual (403 MB) in 71 us, 5.7 TB/s. */
 __device__ __forceinline__ Philox philox(uint64_t low, uint64_t high, uint64_t key) {
     uint32_t c0 = (uint32_t)low, c1 = (uint32_t)(low >> 32), c2 = (uint32_t)high, c3 = (uint32_t)(high >> 32);
     uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
@@ -301,7 +306,10 @@ l3_status launch_dropout(const DropoutArgs& a, bool wide, hipStream_t stream) {
  * runs of V elements; `lanes` lanes (a power of two) take a head, and a slot of them the same pairs of up to
  * `per_slot` heads of one token and tensor, so that sines and cosines are worked out once for these, with all
  * their loads on the way together.  A slot keeps its heads from token to token (the launch's slots are
- * a multiple of a token's), so weights are read, and their gradients kept, once. */
+ * a multiple of a token's), so weights are read, and their gradients kept, once.
+ * Bound by memory: 65536 tokens x 40 heads x 128 turned (1.34 GB) in 245 us, 5.5 TB/s; normalised as well, 40000 x 24 x 64
+ * (246 MB), 59 us, 4.2 TB/s (one head a slot: 122 us); the gradients of 19683 x 18 x 128 (272 MB) 60 us, 4.5 TB/s, and 5 us for
+ * the weights' sums. */
 struct RotateTensor {
     const void* x;
     void* y;
@@ -646,7 +654,7 @@ l3_status run_rotate(l3_ctx* ctx, const l3_rotation* rot, int inverse, float eps
     a.magnitude = rot->magnitude;
     a.eps = eps;
     if (rot->pairs) std::memcpy(a.turns, rot->turns, (size_t)rot->pairs * 8);
-    /* Four heads a slot, where one of them each would still give all CUs their threads */
+    /* Four heads a slot (two for the gradients), where one of them each would give the CUs more threads than they hold */
     const int64_t heads = side[0].heads + side[1].heads;
     const int per_slot = v > 1 && a.tokens * heads * a.lanes >= kManyThreads ? (mode == kNormRotateBack ? 2 : 4) : 1;
     a.q_slots = (side[0].heads + per_slot - 1) / per_slot;
