@@ -11,6 +11,7 @@
  */
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -21,7 +22,6 @@
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -202,34 +202,31 @@ struct Place {
 /* A table entry, held inside the tensor whatever the table says. */
 __device__ __forceinline__ int first_of(const int32_t* first, int i, int tokens) { return min(max(first[i], 0), tokens); }
 
-/* Which tile of which image is the launch's tile number `index`, if every image is cut into tiles of
- * `rows` queries (by_keys: keys)?  64 images at a time, one a lane. */
+/* Which tile of which image is the launch's place number `index`, if every image is cut into tiles of `rows`
+ * queries (by_keys: keys)?  Image i, which starts at token first[i], has the places from first[i] / rows + i on: as many
+ * as it has tiles, or one more, and all can be told from the table without adding tiles up.  64 places of the
+ * table are looked at together, so 64 images take one look, 4096 two. */
 __device__ Place find_tile(const Shape& s, int index, int rows, bool by_keys) {
     const int lane = threadIdx.x & 63;
     Place p = {-1, 0, 0, 0, 0, 0};
     const int32_t* const first = by_keys ? s.kv_first : s.q_first;
     const int tokens = by_keys ? s.kv_tokens : s.q_tokens;
-    int before = 0;
-    for (int i0 = 0; i0 < s.images; i0 += 64) {
-        const int i = i0 + lane;
-        int tiles = 0;
-        if (i < s.images) {
-            const int count = first_of(first, i + 1, tokens) - first_of(first, i, tokens);
-            tiles = count > 0 ? (count + rows - 1) / rows : 0;
-        }
-        int upto = tiles;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
-        }
-        const unsigned long long behind = __ballot(before + upto > index);
-        if (behind) {
-            const int who = __builtin_ctzll(behind);
-            p.image = __builtin_amdgcn_readfirstlane(i0 + who);
-            p.tile = __builtin_amdgcn_readfirstlane(index - before - (__shfl(upto, who) - __shfl(tiles, who)));
-            break;
-        }
-        before += __shfl(upto, 63);
+    int low = 0, high = s.images, found = 0;           /* the image lies in low .. high - 1 */
+    for (;;) {
+        const int step = (high - low + 63) / 64, i = low + lane * step;
+        const int place = i < high ? first_of(first, i, tokens) / rows + i : 0x7FFFFFFF;
+        const unsigned long long upto = __ballot(place <= index);
+        const int count = ~upto ? __builtin_ctzll(~upto) : 64;        /* places ascend */
+        if (count == 0) return p;
+        found = __builtin_amdgcn_readlane(place, count - 1);
+        low += (count - 1) * step;
+        high = min(high, low + step);
+        if (step == 1) break;
+    }
+    const int start = first_of(first, low, tokens), end = first_of(first, low + 1, tokens);
+    if (index - found < (max(end - start, 0) + rows - 1) / rows) {
+        p.image = __builtin_amdgcn_readfirstlane(low);
+        p.tile = __builtin_amdgcn_readfirstlane(index - found);
     }
     if (p.image >= 0) {
         p.q0 = __builtin_amdgcn_readfirstlane(first_of(s.q_first, p.image, s.q_tokens));
@@ -1109,8 +1106,8 @@ Shape shape_of(const l3_attention_shape& s) {
             s.head_dim, s.q_heads, s.kv_heads, s.q_heads / s.kv_heads, (int32_t)s.mask, s.scale, s.cap};
 }
 
-/* Images of `tokens` tokens in all have at most this many tiles of `rows`. */
-int64_t most_tiles(int64_t tokens, int images, int rows) { return tokens / rows + std::min<int64_t>(images, tokens); }
+/* Places that the tiles of `rows` of images of `tokens` tokens in all may have (see find_tile) */
+int64_t most_tiles(int64_t tokens, int images, int rows) { return tokens > 0 ? tokens / rows + images : 0; }
 
 template <typename F>
 void by_width(int head_dim, F f) {

@@ -385,7 +385,7 @@ def test_attention_more_or_fewer_keys(l3, ctx, head_dim, dtype, mask):
     run_attention(l3, ctx, (5, 100, 0, 129, 3, 64), (77, 40, 9, 0, 1, 200), (2, 2), head_dim, dtype, mask, 0.0, mask == 1)
 
 
-@pytest.mark.parametrize("lengths", ((128,), (129,), (257, 255), (640,), tuple([1] * 130), tuple(range(70))))
+@pytest.mark.parametrize("lengths", ((128,), (129,), (257, 255), (640,), tuple([1] * 130), tuple(range(70)), tuple(k % 5 for k in range(1300)), tuple(k % 2 for k in range(4500))))
 def test_attention_lengths(l3, ctx, lengths):
     """Ends of tiles, many images (more than one look at the table), and sums over many tiles."""
     run_attention(l3, ctx, lengths, None, (2, 1), 64, torch.bfloat16, 1, 0.0, False, behind=1 + len(lengths) % 3)
