@@ -18,7 +18,8 @@
  *     rounds in between).
  *   - Sizes and strides are in elements, not bytes, and strides are non-negative.  Rows of an
  *     output must not overlap one another, nor inputs unless a call says so.
- *   - Calls with no work (no tokens, rows or heads) are L3_OK and enqueue nothing.
+ *   - Calls with no work (no tokens, rows or heads) are L3_OK and enqueue nothing, but for gradients
+ *     that are 0 for want of tokens and are written.
  */
 #ifndef L3_TOKENS_H
 #define L3_TOKENS_H
@@ -98,7 +99,7 @@ typedef struct {
 
 /* The first 2*pairs elements of every head are turned, pair j by the angle
  *   2 pi * (position * turns[j] mod 2^64) / 2^64,  pair (a, b) -> magnitude * (a cos - b sin, a sin + b cos);
- * the elements behind them pass through.  Angles are exact to 2^-32 of a turn at any position. */
+ * the elements behind them pass through.  Angles are good to 2^-26 of a turn at any position. */
 typedef struct {
     int32_t         pairs;         /* 0 .. head_dim/2 */
     int32_t         axes;          /* 1: one position per token; 2: the first half of the pairs goes by the
