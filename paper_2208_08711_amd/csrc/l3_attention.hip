@@ -366,38 +366,50 @@ __device__ __forceinline__ void run_wave(Running<DB>& run, const typename HalfVe
         fetch_k(own + stage * 2 * kTile, k + key0 * k_stride, end - key0, lane);
         fetch_v(own + stage * 2 * kTile + kTile, v + key0 * v_stride, end - key0, lane);
     };
+    /* both stages are on their way from the start on: a tile is waited for while the next one's loads, of which
+     * there are kLoads, may still be out */
+    constexpr int kLoads = 2 * Fetch<DB, 32, 64>::kRounds;
+    const auto arrived = [&](int next) {
+        if (next < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else fetched();
+    };
     int stage = 0, key0 = begin + wave * 32;
     fetch(key0, 0);
+    fetch(key0 + WAVES * 32, 1);
     for (; key0 + 32 <= whole; key0 += WAVES * 32, stage ^= 1) {
-        fetched();
-        fetch(key0 + WAVES * 32, stage ^ 1);
+        arrived(key0 + WAVES * 32);
         one_tile<T, DB, 32, CAP, SLOPES, false>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, seen, place, score, lane);
         /* this wave's reads of the tile have come back before the next fetch into it is sent */
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fetch(key0 + 2 * WAVES * 32, stage);
     }
     for (; key0 < end; key0 += WAVES * 32, stage ^= 1) {
-        fetched();
-        fetch(key0 + WAVES * 32, stage ^ 1);
+        arrived(key0 + WAVES * 32);
         one_tile<T, DB, 32, CAP, SLOPES, true>(run, q, reader, own + stage * 2 * kTile, own + stage * 2 * kTile + kTile, key0, seen, place, score, lane);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fetch(key0 + 2 * WAVES * 32, stage);
     }
 }
 
 /* Local memory of a workgroup of WAVES such waves, which what they join takes over */
 template <int DB, int WAVES>
 constexpr int wave_room() {
-    constexpr int tiles = WAVES * 4 * 32 * Tile<DB>::kPitch, join = WAVES * (2 * 32 + 32 * DB * 32) * 4;
+    constexpr int tiles = WAVES * 4 * 32 * Tile<DB>::kPitch, join = (WAVES * (3 * 32 + 32 * (32 * DB + 1)) + 2 * 32) * 4;
     return tiles > join ? tiles : join;
 }
 
 /* The waves' reference points, sums and products joined: store(query, element, product, top, sum) for
- * each of 32 queries and dim elements, the last two the same for all elements of a query. */
+ * each of the first `queries` (of 32) and dim elements, the last two the same for all elements of a query. */
 template <int DB, int WAVES, typename STORE>
-__device__ __forceinline__ void join_waves(const Running<DB>& run, uint8_t* room, int dim, int lane, int wave, STORE store) {
+__device__ __forceinline__ void join_waves(const Running<DB>& run, uint8_t* room, int queries, int dim, int lane, int wave, STORE store) {
+    constexpr int kRow = 32 * DB + 1;                              /* (odd, so that queries lie in different banks) */
     __syncthreads();
-    float* const tops = (float*)room;                              /* [waves][32], then sums, then products */
+    float* const tops = (float*)room;                              /* [waves][32], then sums, factors, */
     float* const sums = tops + WAVES * 32;
-    float* const products = sums + WAVES * 32;                     /* [waves][32 * DB][32] */
+    float* const factors = sums + WAVES * 32;
+    float* const top_of = factors + WAVES * 32;                    /* [32], then the joined sums, */
+    float* const sum_of = top_of + 32;
+    float* const products = sum_of + 32;                           /* [waves][32][kRow] */
     const float sum = across_sum(run.sum);
     if (lane < 32) {
         tops[wave * 32 + lane] = run.top;
@@ -406,22 +418,29 @@ __device__ __forceinline__ void join_waves(const Running<DB>& run, uint8_t* room
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) products[(wave * 32 * DB + 32 * d + acc_row(r, lane >> 5)) * 32 + (lane & 31)] = run.out[d][r];
+        for (int r = 0; r < 16; ++r) products[(wave * 32 + (lane & 31)) * kRow + 32 * d + acc_row(r, lane >> 5)] = run.out[d][r];
     __syncthreads();
-    const int g = threadIdx.x & 31;
-    float top = -kInf, total = 0.0f, f[WAVES];
+    if (threadIdx.x < 32) {
+        const int g = threadIdx.x;
+        float top = -kInf, total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w * 32 + g]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w * 32 + g]);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        f[w] = tops[w * 32 + g] > -kInf ? __builtin_amdgcn_exp2f(tops[w * 32 + g] - top) : 0.0f;
-        total = __builtin_fmaf(f[w], sums[w * 32 + g], total);
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = tops[w * 32 + g] > -kInf ? __builtin_amdgcn_exp2f(tops[w * 32 + g] - top) : 0.0f;
+            factors[w * 32 + g] = f;
+            total = __builtin_fmaf(f, sums[w * 32 + g], total);
+        }
+        top_of[g] = top;
+        sum_of[g] = total;
     }
-    for (int c = threadIdx.x / 32; c < dim; c += WAVES * 2) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < queries * dim; i += WAVES * 64) {
+        const int g = i / dim, c = i - g * dim;
         float x = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) x = __builtin_fmaf(f[w], products[(w * 32 * DB + c) * 32 + g], x);
-        store(g, c, x, top, total);
+        for (int w = 0; w < WAVES; ++w) x = __builtin_fmaf(factors[w * 32 + g], products[(w * 32 + g) * kRow + c], x);
+        store(g, c, x, top_of[g], sum_of[g]);
     }
 }
 
@@ -549,8 +568,7 @@ __global__ __launch_bounds__(kThreads, 1) void l3_attention_few_kernel(ForwardAr
                                     (const T*)a.k.d + (int64_t)p.k0 * a.k.token + (int64_t)kv_head * a.k.head, a.k.token,
                                     (const T*)a.v.d + (int64_t)p.k0 * a.v.token + (int64_t)kv_head * a.v.head, a.v.token, s.head_dim, 0, all, whole, seen,
                                     row + p.m - p.n, score, lane, wave);
-    join_waves<DB, 4>(run, room, s.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
-        if (row0 + g >= p.n) return;
+    join_waves<DB, 4>(run, room, min(32, p.n - row0), s.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
         const bool any = seen_by(s, p, prefix, row0 + g) > 0;
         ((T*)const_cast<void*>(a.out.d))[(int64_t)(p.q0 + row0 + g) * a.out.token + (int64_t)head * a.out.head + c] = (T)(any ? x / total : 0.0f);
         if (c == 0 && a.lse) a.lse[(int64_t)head * s.q_tokens + p.q0 + row0 + g] = any ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -kInf;
@@ -984,7 +1002,9 @@ struct StepArgs {
 /* A workgroup takes `chunk` keys of one sequence and key head, against up to 32 of the query heads
  * that share them (one a lane); its waves take tiles in turn, each on its own, and join at the end.  Bound by
  * memory: 32 caches of 512 to 32768 tokens x 8 heads x 128 (2.29 GB) in 440 us, 5.2 TB/s, what a copy reaches; with the
- * heads' workgroups far apart in the launch 556 us (rows of 256 bytes 2 KB apart), in pieces four times as long 567. */
+ * heads' workgroups far apart in the launch 556 us (rows of 256 bytes 2 KB apart), in pieces four times as long 567.  Few
+ * caches are their workgroups' starts and ends: one of 32768 x 8 heads x 128 (134 MB) 40 us with the join, one of 131072 x 1 head
+ * (67 MB) 25, one of 1000 x 8 12.5. */
 template <typename T, int DB, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(StepArgs a) {
     constexpr int kTile = kStepKeys * Tile<DB>::kPitch;
@@ -998,7 +1018,7 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
     at /= a.blocks_of_heads;
     const int chunk = at % a.chunks, sequence = at / a.chunks;
     const int length = __builtin_amdgcn_readfirstlane(min(max(a.lengths[sequence], 0), a.max_length));
-    const int begin = chunk * a.chunk, end = min(begin + a.chunk, length);
+    const int begin = chunk * a.chunk, end = (int)min((int64_t)begin + a.chunk, (int64_t)length);
     const int in_group = of * 32 + (lane & 31), head = kv_head * a.group + in_group;
     const bool there = in_group < a.group;
     if (begin >= length && chunk > 0) return;
@@ -1013,8 +1033,7 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
     run.start();
     run_wave<T, DB, CAP, SLOPES, kStepWaves>(run, q, lds_address(room) + wave * 4 * kTile, k, a.k.token, v, a.v.token, a.head_dim, begin, end, end, end,
                                              length - 1, score, lane, wave);
-    join_waves<DB, kStepWaves>(run, room, a.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
-        if (of * 32 + g >= a.group) return;
+    join_waves<DB, kStepWaves>(run, room, min(32, a.group - of * 32), a.head_dim, lane, wave, [&](int g, int c, float x, float top, float total) {
         const int64_t h = kv_head * a.group + of * 32 + g;
         if (!a.partial) {
             ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + h * a.out.head + c] = (T)(length > 0 ? x / total : 0.0f);
@@ -1029,38 +1048,62 @@ __global__ __launch_bounds__(kStepThreads, 1) void l3_attention_step_kernel(Step
     });
 }
 
-/* The chunks of a sequence and head joined; one workgroup a head, one thread an element. */
-template <typename T>
-__global__ __launch_bounds__(L3_MAX_HEAD_DIM) void l3_attention_join_kernel(StepArgs a) {
-    const int sequence = blockIdx.x / a.q_heads, head = blockIdx.x - sequence * a.q_heads, c = threadIdx.x;
+/* The chunks of a sequence and head joined by one workgroup: first every chunk's factor, a chunk a
+ * thread, then the products, ROWS chunks side by side and sixteen loads of each on the way, no branch between
+ * them (131072 tokens of one head in 512 chunks: 23 us with branches, 7 without).  ROWS: 8, or 1 where a few chunks
+ * are all there are. */
+constexpr int kFewChunks = 32;
+
+template <typename T, int ROWS>
+__global__ __launch_bounds__(ROWS * L3_MAX_HEAD_DIM) void l3_attention_join_kernel(StepArgs a) {
+    constexpr int kJoinRows = ROWS, kJoinThreads = ROWS * L3_MAX_HEAD_DIM, kMost = ROWS > 1 ? kStepGrid : kFewChunks;
+    __shared__ float factors[kMost], room[kJoinThreads], most[kJoinThreads / 64];
+    const int sequence = blockIdx.x / a.q_heads, head = blockIdx.x - sequence * a.q_heads;
     const int length = min(max(a.lengths[sequence], 0), a.max_length);
     const int chunks = (length + a.chunk - 1) / a.chunk;
-    if (c >= a.head_dim) return;
     const int64_t pitch = a.head_dim + kStepRecord;
     const float* const record = a.partial + ((int64_t)sequence * a.q_heads + head) * a.chunks * pitch;
-    /* four chunks at a time, so that their loads travel together */
-    float top = -kInf, total = 0.0f, x = 0.0f;
-    for (int i = 0; i < chunks; i += 4) {
-        float tops[4], sums[4], parts[4];
+    const int t = threadIdx.x, c = t % L3_MAX_HEAD_DIM, r = t / L3_MAX_HEAD_DIM;
+
+    /* (there are at most kMost chunks: kEach a thread, whose tops and sums stay in registers) */
+    constexpr int kEach = (kMost + kJoinThreads - 1) / kJoinThreads;
+    float top = -kInf, total = 0.0f, tops[kEach], sums[kEach];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float* const r = record + min(i + k, chunks - 1) * pitch;
-            tops[k] = i + k < chunks ? r[0] : -kInf;
-            sums[k] = r[1];
-            parts[k] = r[kStepRecord + c];
-        }
-        const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), next = fmaxf(top, most);
-        const float shrink = top > -kInf ? __builtin_amdgcn_exp2f(top - next) : 0.0f;
-        total *= shrink;
-        x *= shrink;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float f = tops[k] > -kInf ? __builtin_amdgcn_exp2f(tops[k] - next) : 0.0f;
-            total = __builtin_fmaf(f, sums[k], total);
-            x = __builtin_fmaf(f, parts[k], x);
-        }
-        top = next;
+    for (int k = 0; k < kEach; ++k) {
+        const int i = t + k * kJoinThreads;
+        tops[k] = i < chunks ? record[i * pitch] : -kInf;
+        sums[k] = i < chunks ? record[i * pitch + 1] : 0.0f;
+        top = fmaxf(top, tops[k]);
     }
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (t % 64 == 0) most[t / 64] = top;
+    __syncthreads();
+    for (int w = 0; w < kJoinThreads / 64; ++w) top = fmaxf(top, most[w]);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = t + k * kJoinThreads;
+        const float f = tops[k] == -kInf ? 0.0f : __builtin_amdgcn_exp2f(tops[k] - top);
+        if (i < chunks) factors[i] = f;
+        total = __builtin_fmaf(f, sums[k], total);
+    }
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    __syncthreads();
+    if (t % 64 == 0) most[t / 64] = total;
+    float x = 0.0f;
+    const int element = kStepRecord + min(c, a.head_dim - 1);
+    for (int i = r; i < chunks; i += 16 * kJoinRows) {
+        float part[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) part[k] = record[min(i + k * kJoinRows, chunks - 1) * pitch + element];   /* (no branch between loads) */
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x = __builtin_fmaf(i + k * kJoinRows < chunks ? factors[i + k * kJoinRows] : 0.0f, part[k], x);
+    }
+    room[t] = x;
+    __syncthreads();
+    if (r || c >= a.head_dim) return;
+    for (int k = 1; k < kJoinRows; ++k) x += room[k * L3_MAX_HEAD_DIM + c];
+    total = 0.0f;
+    for (int w = 0; w < kJoinThreads / 64; ++w) total += most[w];
     ((T*)const_cast<void*>(a.out.d))[(int64_t)sequence * a.out.token + (int64_t)head * a.out.head + c] = (T)(chunks > 0 ? x / total : 0.0f);
 }
 
@@ -1231,7 +1274,9 @@ l3_status run_step(const StepArgs& a, hipStream_t stream) {
             ok = launch(l3_attention_step_kernel<T, db.value, cap.value, slopes.value>, grid, kStepThreads, 0, stream, a);
         });
     });
-    if (ok && a.partial) ok = launch(l3_attention_join_kernel<T>, (int64_t)a.n * a.q_heads, L3_MAX_HEAD_DIM, 0, stream, a);
+    if (ok && a.partial)
+        ok = a.chunks <= kFewChunks ? launch(l3_attention_join_kernel<T, 1>, (int64_t)a.n * a.q_heads, L3_MAX_HEAD_DIM, 0, stream, a)
+                                    : launch(l3_attention_join_kernel<T, 8>, (int64_t)a.n * a.q_heads, 8 * L3_MAX_HEAD_DIM, 0, stream, a);
     return status_of(ok);
 }
 

@@ -554,9 +554,9 @@ __global__ __launch_bounds__(kRotateThreads) void l3_weight_grad_kernel(const fl
         for (int b = r; b < blocks; b += 8 * kRows) {
             float part[8];                                         /* eight loads on the way together */
 #pragma unroll
-            for (int i = 0; i < 8; ++i) part[i] = b + i * kRows < blocks ? partial[(int64_t)(b + i * kRows) * 2 * head_dim + column] : 0.0f;
+            for (int i = 0; i < 8; ++i) part[i] = partial[(int64_t)min(b + i * kRows, blocks - 1) * 2 * head_dim + column];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += part[i];
+            for (int i = 0; i < 8; ++i) s += b + i * kRows < blocks ? part[i] : 0.0f;
         }
     room[r][c] = s;
     __syncthreads();
