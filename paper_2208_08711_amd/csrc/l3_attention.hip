@@ -80,7 +80,7 @@ __device__ __forceinline__ uint32_t row_place(int lane) {
 }
 template <typename T, int DB>
 __device__ __forceinline__ typename HalfVec<T, 8>::type read_row(uint32_t at, int block, int step) {
-    return __builtin_bit_cast(typename HalfVec<T, 8>::type, *(const lds_u32x4*)((at ^ (step * 32)) + block * 32 * Tile<DB>::kPitch));
+    return __builtin_bit_cast(typename HalfVec<T, 8>::type, *(const lds_u32x4*)(uintptr_t)((at ^ (step * 32)) + block * 32 * Tile<DB>::kPitch));
 }
 
 /* A lane's places for operand columns: of column 32*db + (lane & 31) the rows row0 + 4*half + {0..3, 8..11},
@@ -103,7 +103,7 @@ template <typename T, int DB>
 __device__ __forceinline__ typename HalfVec<T, 8>::type read_columns(const ColumnPlace& p, int row0, int db) {
     s16x4 part[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((p.at[u] ^ (db * 64)) + row0 * Tile<DB>::kPitch));
+    for (int u = 0; u < 2; ++u) part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((p.at[u] ^ (db * 64)) + row0 * Tile<DB>::kPitch));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(typename HalfVec<T, 8>::type, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -117,16 +117,13 @@ struct Reader {
     __device__ __forceinline__ explicit Reader(int lane) : row(row_place<DB>(lane)), column(column_place<DB>(lane)) {}
 };
 
-/* Format word of an untyped buffer descriptor. */
-constexpr int kBufferFlags = 0x00020000;
-
 /* BYTES (4 or 16) a lane from byte `offset` of a buffer of `size` bytes at `base` to local memory: the wave's
  * lanes one after the other from `lds` on; 0 for what lies outside.  base, size, lds: the wave's.
  * (The descriptor's type exists in the device's compilation only.) */
 template <int BYTES>
 __device__ __forceinline__ void buffer_to_lds(uint32_t lds, const void* base, int32_t size, uint32_t offset) {
 #ifdef __HIP_DEVICE_COMPILE__
-    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, size, kBufferFlags);
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, size, 0x00020000 /* untyped */);
     if (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void*)(uintptr_t)lds, 16, offset, 0, 0, 0);
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void*)(uintptr_t)lds, 4, offset, 0, 0, 0);
 #endif
